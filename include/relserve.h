@@ -309,6 +309,35 @@ int32_t relserve_linear_w8a8(const void* a, const void* w, const float* w_scale,
                              int32_t T, int32_t N, int32_t K, int32_t epilogue, const void* residual, void* out,
                              float out_scale, int32_t packed, void* stream);
 
+/* ---- 8-bit integer projections with a scale for each token and each output channel (a variant beside the paper's 16-bit models, as
+ * relserve_layer_weights_w8a8 is, without calibration: a token's scale is taken from the token itself) ----
+ * Row t of codes [T, n] (int8) with scales [T] (fp32) stands for codes[t, i] * scales[t].  A row is made with
+ *     scale = m / 127, m = the row's largest magnitude;  code = the integer nearest to value * 127 / m (ties to even)
+ * so codes lie in [-127, 127].  A row of zeros has scale 0 and codes of 0; one with a NaN or an infinity has a scale that is not finite
+ * and codes of 0: whatever is computed from it is not finite either.
+ * All pointers are device memory: rows of values and weights and the codes 16-byte aligned (RELSERVE_ERR_BAD_ARGUMENT otherwise).
+ *
+ * relserve_quantise_rows_i8: codes and scales of the rows of in [n_rows, n] bf16 (activations, or weights: rows are output channels).
+ * n a multiple of 8.
+ *
+ * relserve_add_rmsnorm_i8: the norm in front of a projection, with the residual's addition ahead of it.  s = x + delta, rounded to x's
+ * type (bf16, or fp32 when x_is_f32); delta bf16 or NULL (s = x).  sum, if not NULL, receives s; it may be x, and overlaps nothing else.
+ * codes, scales: of s * w / sqrt(mean(s^2) + eps), sums in fp32 as relserve_rmsnorm.  hidden a multiple of 8.
+ *
+ * relserve_linear_i8: out[t, n] = (sum_k a[t, k] * w[n, k]) * (w_scale[n] * a_scale[t]): a [T, K], w [N, K] int8 (any codes, -128 too),
+ * the sum exact in 32 bits (and so the same bits whatever tiles and splits compute it), then fp32; epilogues, residuals and outputs as
+ * relserve_linear.  K a multiple of 128, at most 130944 (RELSERVE_ERR_TOO_LARGE above), N of 4 (of 16 for SwiGLU).  packed != 0: w is
+ * relserve_pack_weight applied to the matrix seen as [N, K / 2] two-byte units.  workspace: scratch as in relserve_layer_step, of at least
+ * relserve_linear_i8_workspace_bytes(T, N) bytes: lets the k range of a few tokens' product be computed by several workgroups; or NULL (few
+ * tokens are then slower). */
+int32_t relserve_quantise_rows_i8(const void* in, int32_t n_rows, int32_t n, void* codes, float* scales, void* stream);
+int32_t relserve_add_rmsnorm_i8(const void* x, int32_t x_is_f32, const void* delta, const void* w, float eps, int32_t n_rows,
+                                int32_t hidden, void* sum, void* codes, float* scales, void* stream);
+int32_t relserve_linear_i8_workspace_bytes(int32_t T, int32_t N, size_t* out);
+int32_t relserve_linear_i8(const void* a, const float* a_scale, const void* w, const float* w_scale, int32_t T, int32_t N, int32_t K,
+                           int32_t epilogue, const void* residual, void* out, int32_t packed, void* workspace, size_t workspace_bytes,
+                           void* stream);
+
 /* out[T, N] = a[T, K] * w[N, K]^T (Eq. 3 and every other dense map), bf16 in,
  * fp32 accumulate.  epilogue: 0 = store bf16; 1 = add residual (bf16 [T, N],
  * or none when NULL) and store fp32; 2 = add residual (fp32 [T, N]) and store bf16; 3 = SwiGLU:

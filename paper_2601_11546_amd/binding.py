@@ -38,7 +38,8 @@ EXPORTS = ["relserve_version", "relserve_strerror", "relserve_config_validate", 
            "relserve_duration_fit", "relserve_duration_predict", "relserve_batch_decompose", "relserve_pem_estimate",
            "relserve_aba_decide", "relserve_starved_priority", "relserve_static_priority", "relserve_utok_estimate",
            "relserve_priority_reuse", "relserve_prefill_candidate",
-           "relserve_layer_step_w8a8", "relserve_model_step_w8a8", "relserve_rmsnorm_codes", "relserve_quantise_bf16", "relserve_linear_w8a8"]
+           "relserve_layer_step_w8a8", "relserve_model_step_w8a8", "relserve_rmsnorm_codes", "relserve_quantise_bf16", "relserve_linear_w8a8",
+           "relserve_quantise_rows_i8", "relserve_add_rmsnorm_i8", "relserve_linear_i8", "relserve_linear_i8_workspace_bytes"]
 
 
 class RelserveError(RuntimeError):
@@ -143,6 +144,12 @@ for _n, _a in {
     "relserve_quantise_bf16": [C.c_void_p, C.c_int64, C.c_float, C.c_void_p, C.c_void_p],
     "relserve_linear_w8a8": [C.c_void_p, C.c_void_p, C.c_void_p, C.c_float, C.c_int32, C.c_int32, C.c_int32, C.c_int32,
                              C.c_void_p, C.c_void_p, C.c_float, C.c_int32, C.c_void_p],
+    "relserve_quantise_rows_i8": [C.c_void_p, C.c_int32, C.c_int32, C.c_void_p, C.c_void_p, C.c_void_p],
+    "relserve_add_rmsnorm_i8": [C.c_void_p, C.c_int32, C.c_void_p, C.c_void_p, C.c_float, C.c_int32, C.c_int32, C.c_void_p, C.c_void_p,
+                                C.c_void_p, C.c_void_p],
+    "relserve_linear_i8_workspace_bytes": [C.c_int32, C.c_int32, C.c_void_p],
+    "relserve_linear_i8": [C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_int32, C.c_int32, C.c_int32, C.c_int32, C.c_void_p,
+                           C.c_void_p, C.c_int32, C.c_void_p, C.c_size_t, C.c_void_p],
     "relserve_model_workspace_bytes": [C.c_void_p, C.c_int32, C.c_int32, C.c_void_p],
     "relserve_model_step": [C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_size_t,
                             C.c_void_p],
@@ -373,10 +380,10 @@ def relserve_linear_w8a8(a, w, w_scale, a_scale: float, epilogue: int, residual,
 
 
 def pack_codes(w):
-    """An [N, K] uint8 code matrix in the packed layout: relserve_pack_weight on its rows seen as K / 2 two-byte units."""
+    """An [N, K] code matrix (uint8, or the int8 projections' integers) in the packed layout: relserve_pack_weight on its rows seen as K / 2 two-byte units."""
     import torch
     n, k = w.shape
-    packed = torch.empty(relserve_packed_weight_elems(n, k // 2) * 2, dtype=torch.uint8, device=w.device)
+    packed = torch.empty(relserve_packed_weight_elems(n, k // 2) * 2, dtype=w.dtype, device=w.device)
     _check(_lib.relserve_pack_weight(_ptr(w), n, k // 2, _ptr(packed), _stream(None)), "relserve_pack_weight")
     return packed
 
@@ -387,6 +394,60 @@ def pack_layer_weights_w8a8(weights: dict) -> dict:
         out[name] = pack_codes(weights[name])
     out["packed"] = True
     return out
+
+
+def _dense(where: str, **tensors) -> None:
+    """The int8 entry points take whole row-major matrices on one device, of the types and shapes named: (tensor, dtype, shape) each."""
+    device = None
+    for name, (t, dtype, shape) in tensors.items():
+        if t is None:
+            continue
+        if t.dtype != dtype or t.shape != shape or not t.is_contiguous():
+            raise ValueError(f"{where}: {name} must be a contiguous {dtype} tensor of shape {tuple(shape)}, "
+                             f"not {t.dtype} {tuple(t.shape)} with strides {t.stride()}")
+        device = device or t.device
+        if t.device != device:
+            raise ValueError(f"{where}: {name} lies on {t.device}, not on {device}")
+    if device.type != "cuda" or device.index != torch.cuda.current_device():
+        raise ValueError(f"{where}: the tensors lie on {device}, which is not the current device")
+
+
+def relserve_quantise_rows_i8(values, codes, scales, stream=None) -> None:
+    """codes [T, n] int8, scales [T] fp32 of the rows of values [T, n] bf16."""
+    _dense("relserve_quantise_rows_i8", values=(values, torch.bfloat16, values.shape), codes=(codes, torch.int8, values.shape),
+           scales=(scales, torch.float32, values.shape[:1]))
+    _check(_lib.relserve_quantise_rows_i8(_ptr(values), values.shape[0], values.shape[1], _ptr(codes), _ptr(scales), _stream(stream)),
+           "relserve_quantise_rows_i8")
+
+
+def relserve_add_rmsnorm_i8(x, w, eps: float, codes, scales, delta=None, sum_out=None, stream=None) -> None:
+    """codes [T, H] int8, scales [T] fp32 of the normed x + delta (x bf16 or fp32, delta bf16); sum_out (may be x): x + delta."""
+    f32 = x.dtype == torch.float32
+    _dense("relserve_add_rmsnorm_i8", x=(x, torch.float32 if f32 else torch.bfloat16, x.shape), w=(w, torch.bfloat16, x.shape[1:]),
+           codes=(codes, torch.int8, x.shape), scales=(scales, torch.float32, x.shape[:1]), delta=(delta, torch.bfloat16, x.shape),
+           sum_out=(sum_out, x.dtype, x.shape))
+    _check(_lib.relserve_add_rmsnorm_i8(_ptr(x), int(f32), _ptr(delta), _ptr(w), float(eps), x.shape[0], x.shape[1], _ptr(sum_out),
+                                        _ptr(codes), _ptr(scales), _stream(stream)), "relserve_add_rmsnorm_i8")
+
+
+def relserve_linear_i8_workspace_bytes(tokens: int, n: int) -> int:
+    out = C.c_size_t()
+    _check(_lib.relserve_linear_i8_workspace_bytes(int(tokens), int(n), C.byref(out)), "relserve_linear_i8_workspace_bytes")
+    return int(out.value)
+
+
+def relserve_linear_i8(a, a_scale, w, w_scale, epilogue: int, residual, out, n: int = 0, workspace=None, stream=None) -> None:
+    """a [T, K], w [N, K] int8 codes (n > 0: w is packed by pack_codes and has n rows), a_scale [T], w_scale [N] fp32.
+    workspace: uint8 tensor of relserve_linear_i8_workspace_bytes(T, N) bytes or more, or None."""
+    t, k = a.shape
+    rows = int(n) if n else w.shape[0]
+    _dense("relserve_linear_i8", a=(a, torch.int8, a.shape), a_scale=(a_scale, torch.float32, a.shape[:1]),
+           w=(w, torch.int8, ((rows + 255) // 256 * 256 * k,) if n else (rows, k)), w_scale=(w_scale, torch.float32, (rows,)),
+           out=(out, torch.float32 if epilogue == 1 else torch.bfloat16, (t, rows // 2 if epilogue == 3 else rows)),
+           residual=(residual, torch.bfloat16 if epilogue == 1 else torch.float32, (t, rows)))
+    _check(_lib.relserve_linear_i8(_ptr(a), _ptr(a_scale), _ptr(w), _ptr(w_scale), t, rows, k, int(epilogue), _ptr(residual), _ptr(out),
+                                   int(n > 0), _ptr(workspace), 0 if workspace is None else workspace.numel() * workspace.element_size(),
+                                   _stream(stream)), "relserve_linear_i8")
 
 
 def relserve_static_scratch_bytes() -> int:

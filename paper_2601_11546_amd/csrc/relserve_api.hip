@@ -3,6 +3,7 @@
 #include <algorithm>
 #include <cmath>
 #include <cstring>
+#include <initializer_list>
 #include <mutex>
 #include <new>
 
@@ -658,6 +659,16 @@ int32_t relserve::expand_batch(const relserve_layer_config& cfg, const relserve_
 // behind (the runtime keeps the last one until it is read) must not be taken for theirs.
 static inline void drop_stale_hip_error() { (void)hipGetLastError(); }
 
+// Operands that kernels read and write 16 bytes at a time (null: not given).
+static inline bool aligned16(std::initializer_list<const void*> pointers) {
+    for (const void* p : pointers)
+        if (reinterpret_cast<uintptr_t>(p) % 16) return false;
+    return true;
+}
+
+// Sums of products of 8-bit integers stay inside 32 bits: 2^14 K < 2^31.
+static constexpr int32_t kMaxKInt8 = 131072 - 128;
+
 extern "C" {
 
 int32_t relserve_version(void) { return 100; }
@@ -1165,6 +1176,56 @@ int32_t relserve_linear_w8a8(const void* a, const void* w, const float* w_scale,
     const CodeScales codes{w_scale, a_scale, out_scale};
     hipError_t e = launch_linear(a, w, T, N, K, epilogue, residual, out, static_cast<hipStream_t>(stream), nullptr, packed != 0, &codes);
     return e == hipSuccess ? RELSERVE_OK : RELSERVE_ERR_HIP;
+}
+
+int32_t relserve_quantise_rows_i8(const void* in, int32_t n_rows, int32_t n, void* codes, float* scales, void* stream) {
+    drop_stale_hip_error();
+    if (n_rows < 0 || n <= 0 || n % 8) return RELSERVE_ERR_BAD_ARGUMENT;
+    if (n_rows == 0) return RELSERVE_OK;
+    if (!in || !codes || !scales) return RELSERVE_ERR_NULL_POINTER;
+    if (!aligned16({in, codes})) return RELSERVE_ERR_BAD_ARGUMENT;
+    return launch_row_codes(in, false, nullptr, nullptr, 0.0f, n_rows, n, nullptr, codes, scales, static_cast<hipStream_t>(stream)) == hipSuccess
+               ? RELSERVE_OK
+               : RELSERVE_ERR_HIP;
+}
+
+int32_t relserve_add_rmsnorm_i8(const void* x, int32_t x_is_f32, const void* delta, const void* w, float eps, int32_t n_rows,
+                                int32_t hidden, void* sum, void* codes, float* scales, void* stream) {
+    drop_stale_hip_error();
+    if (n_rows < 0 || hidden <= 0 || hidden % 8) return RELSERVE_ERR_BAD_ARGUMENT;
+    if (n_rows == 0) return RELSERVE_OK;
+    if (!x || !w || !codes || !scales) return RELSERVE_ERR_NULL_POINTER;
+    if (!aligned16({x, delta, w, sum, codes})) return RELSERVE_ERR_BAD_ARGUMENT;
+    return launch_row_codes(x, x_is_f32 != 0, delta, w, eps, n_rows, hidden, sum, codes, scales, static_cast<hipStream_t>(stream)) == hipSuccess
+               ? RELSERVE_OK
+               : RELSERVE_ERR_HIP;
+}
+
+int32_t relserve_linear_i8_workspace_bytes(int32_t T, int32_t N, size_t* out) {
+    if (!out) return RELSERVE_ERR_NULL_POINTER;
+    if (T < 0 || N <= 0) return RELSERVE_ERR_BAD_ARGUMENT;
+    *out = (size_t)gemm_scratch_floats(T, N) * 4;
+    return RELSERVE_OK;
+}
+
+int32_t relserve_linear_i8(const void* a, const float* a_scale, const void* w, const float* w_scale, int32_t T, int32_t N, int32_t K,
+                           int32_t epilogue, const void* residual, void* out, int32_t packed, void* workspace, size_t workspace_bytes,
+                           void* stream) {
+    drop_stale_hip_error();
+    if (T < 0 || N <= 0 || K <= 0 || K % 128 || epilogue < 0 || epilogue > 3) return RELSERVE_ERR_BAD_ARGUMENT;
+    if (epilogue == 3 ? N % 16 : N % 4) return RELSERVE_ERR_BAD_ARGUMENT;
+    const int64_t w_rows = packed ? ((int64_t)N + 255) / 256 * 256 : N;
+    if (K > kMaxKInt8 || (int64_t)T * K >= ((int64_t)1 << 31) || w_rows * K >= ((int64_t)1 << 31)) return RELSERVE_ERR_TOO_LARGE;
+    if (T == 0) return RELSERVE_OK;
+    if (!a || !a_scale || !w || !w_scale || !out) return RELSERVE_ERR_NULL_POINTER;
+    if (epilogue == 2 && !residual) return RELSERVE_ERR_NULL_POINTER;
+    if (!aligned16({a, w, w_scale, residual, out})) return RELSERVE_ERR_BAD_ARGUMENT;
+    if (workspace && (reinterpret_cast<uintptr_t>(workspace) % kAlign || workspace_bytes < (size_t)gemm_scratch_floats(T, N) * 4))
+        return RELSERVE_ERR_WORKSPACE;
+    return launch_linear_i8(a, a_scale, w, w_scale, T, N, K, epilogue, residual, out, static_cast<hipStream_t>(stream),
+                            static_cast<float*>(workspace), packed != 0) == hipSuccess
+               ? RELSERVE_OK
+               : RELSERVE_ERR_HIP;
 }
 
 int32_t relserve_static_scratch_bytes(size_t* out) {

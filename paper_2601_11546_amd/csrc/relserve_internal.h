@@ -192,6 +192,13 @@ struct KvFormat {
 hipError_t launch_qkv_rope_append(const BatchDev& b, const relserve_layer& L, const void* h, const void* w_qkv,
                                   void* q_out, void* k_pages, void* v_pages, hipStream_t s, float* accum = nullptr,
                                   bool w_packed = false, KvFormat kv = KvFormat{}, const CodeScales* codes = nullptr);
+// Rows as 8-bit integers with a scale each: of rmsnorm(x + delta) * w (delta may be null; sum, if given, receives x + delta in x's type),
+// or, w null, of x itself.
+hipError_t launch_row_codes(const void* x, bool x_is_f32, const void* delta, const void* w, float eps, int32_t rows, int32_t n, void* sum,
+                            void* codes, float* scales, hipStream_t s);
+// launch_linear on 8-bit integers a [T, K], w [N, K] (K % 128 == 0) with a scale for each row of either
+hipError_t launch_linear_i8(const void* a, const float* a_scale, const void* w, const float* w_scale, int32_t T, int32_t N, int32_t K,
+                            int32_t epilogue, const void* residual, void* out, hipStream_t s, float* accum, bool w_packed);
 // bf16 [n] -> 8-bit codes of value / scale (n % 8 == 0)
 hipError_t launch_quantise_bf16(const void* in, int64_t n, float scale, void* codes, hipStream_t s);
 // Attention passes; part_o [T + split_slot_cap(T), n_q, d] fp32 and part_ml [.., n_q, 2] fp32 hold the prefix partials
