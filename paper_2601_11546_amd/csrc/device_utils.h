@@ -109,4 +109,11 @@ __device__ __forceinline__ f32x4_t mfma_16x16x128_f8(i32x8_t a, i32x8_t b, f32x4
     return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, b, c, 0, 0, 0, 0, 0, 0);
 }
 
+// The same of 8-bit integers, exact 32-bit sums: two products of k = 64, whose operand is 16 codes a lane.  One behind the other on the same
+// sums is the fastest order: 3.93 POP/s with all CUs on register operands, all first halves and then all second ones 3.12, 32 x 32 x 32 3.27.
+__device__ __forceinline__ i32x4_t mfma_16x16x128_i8(i32x8_t a, i32x8_t b, i32x4_t c) {
+    c = __builtin_amdgcn_mfma_i32_16x16x64_i8(__builtin_shufflevector(a, a, 0, 1, 2, 3), __builtin_shufflevector(b, b, 0, 1, 2, 3), c, 0, 0, 0);
+    return __builtin_amdgcn_mfma_i32_16x16x64_i8(__builtin_shufflevector(a, a, 4, 5, 6, 7), __builtin_shufflevector(b, b, 4, 5, 6, 7), c, 0, 0, 0);
+}
+
 }  // namespace relserve

@@ -151,7 +151,8 @@ hipError_t launch_rope_append(const BatchDev& b, const relserve_layer& L, void* 
 // lets skinny problems (T <= 256), narrow outputs at mid-size T and the incomplete last round of larger
 // ones split K over workgroups (partial tiles written there, summed by a second kernel).
 int64_t gemm_scratch_floats(int64_t T, int64_t n_max);
-void gemm_force_plan(int cand, int splits);   // test hook, see relserve_debug_force_gemm_plan
+void gemm_force_plan(int cand, int splits);      // test hook, see relserve_debug_force_gemm_plan
+void gemm_force_plan_i8(int cand, int splits);   // its part for the int8 projections
 // How a projection of more tokens than SKINNY_MAX_T is tiled (host arithmetic alone): tiles of rows tokens x cols features,
 // of which the last tail_tiles split their k range `splits` ways.  K counts 2-byte units, so half of it for 8-bit codes.
 // Where nothing is split and cols1 > 0 it is two launches: the first cols1 columns of tiles on rows1 tokens each, the others on rows2
@@ -199,6 +200,10 @@ hipError_t launch_row_codes(const void* x, bool x_is_f32, const void* delta, con
 // launch_linear on 8-bit integers a [T, K], w [N, K] (K % 128 == 0) with a scale for each row of either
 hipError_t launch_linear_i8(const void* a, const float* a_scale, const void* w, const float* w_scale, int32_t T, int32_t N, int32_t K,
                             int32_t epilogue, const void* residual, void* out, hipStream_t s, float* accum, bool w_packed);
+// launch_qkv_rope_append on 8-bit integers h [T, H] and w_qkv, with a scale for each row of either
+hipError_t launch_qkv_rope_append_i8(const BatchDev& b, const relserve_layer& L, const void* h, const float* h_scale, const void* w_qkv,
+                                     const float* w_scale, void* q_out, void* k_pages, void* v_pages, hipStream_t s, float* accum,
+                                     bool w_packed, KvFormat kv);
 // bf16 [n] -> 8-bit codes of value / scale (n % 8 == 0)
 hipError_t launch_quantise_bf16(const void* in, int64_t n, float scale, void* codes, hipStream_t s);
 // Attention passes; part_o [T + split_slot_cap(T), n_q, d] fp32 and part_ml [.., n_q, 2] fp32 hold the prefix partials

@@ -234,6 +234,23 @@ def test_linear_swiglu(rs, t, inner, k, packed):
     assert torch.equal(p.check(3, p.workspace()), p.check(3, None))
 
 
+@pytest.mark.parametrize("splits", [0, 2, 4])
+@pytest.mark.parametrize("tile", range(5))
+def test_every_tile_and_split_gives_the_same_bits(rs, tile, splits):
+    p, q = Product(rs, 700, 1284, 4096, True), Product(rs, 333, 1008, 4096, False)
+    want = [(x, e, x.check(e, x.workspace())) for x, e in ((p, 0), (p, 1), (p, 2), (q, 3), (q, 0))]
+    try:
+        for x, e, w in want:
+            print(f"[case] linear i8 T={x.t} N={x.n} epilogue {e} tile {tile} splits {splits}", flush=True)
+            rs.relserve_debug_force_gemm_plan(tile, splits)
+            got = x.check(e, x.workspace())
+            rs.relserve_debug_force_gemm_plan()
+            if e in (0, 3):     # (the others' residuals are drawn anew)
+                assert torch.equal(got, w)
+    finally:
+        rs.relserve_debug_force_gemm_plan()
+
+
 @pytest.mark.parametrize("t", [1, 40, 300])
 def test_largest_sums(rs, t):
     """Codes at the ends of their range, k as long as 32 bits allow: sums up to 2^31 - 2^21."""
