@@ -396,38 +396,50 @@ def pack_layer_weights_w8a8(weights: dict) -> dict:
     return out
 
 
-def _dense(where: str, **tensors) -> None:
-    """The int8 entry points take whole row-major matrices on one device, of the types and shapes named: (tensor, dtype, shape) each."""
+def _dense(where: str, *tensors) -> None:
+    """The int8 entry points take whole row-major matrices on the current device, of the types and shapes named: (name, tensor, dtype, shape)."""
     device = None
-    for name, (t, dtype, shape) in tensors.items():
+    for name, t, dtype, shape in tensors:
         if t is None:
             continue
-        if t.dtype != dtype or t.shape != shape or not t.is_contiguous():
+        if t.dtype is not dtype or t.shape != shape or not t.is_contiguous():
             raise ValueError(f"{where}: {name} must be a contiguous {dtype} tensor of shape {tuple(shape)}, "
                              f"not {t.dtype} {tuple(t.shape)} with strides {t.stride()}")
-        device = device or t.device
-        if t.device != device:
-            raise ValueError(f"{where}: {name} lies on {t.device}, not on {device}")
-    if device.type != "cuda" or device.index != torch.cuda.current_device():
-        raise ValueError(f"{where}: the tensors lie on {device}, which is not the current device")
+        if device is None:
+            device = t.get_device()
+        elif t.get_device() != device:
+            raise ValueError(f"{where}: {name} lies on {t.device}, other tensors elsewhere")
+    if device < 0 or device != torch.cuda.current_device():
+        raise ValueError(f"{where}: the tensors do not lie on the current device")
+
+
+def _address(t):
+    return None if t is None else t.data_ptr()
+
+
+def _stream_address(t, stream):
+    """The stream's handle; by default that of the current stream of t's device (checked to be the current one)."""
+    return stream.cuda_stream if stream is not None else torch._C._cuda_getCurrentRawStream(t.get_device())
 
 
 def relserve_quantise_rows_i8(values, codes, scales, stream=None) -> None:
     """codes [T, n] int8, scales [T] fp32 of the rows of values [T, n] bf16."""
-    _dense("relserve_quantise_rows_i8", values=(values, torch.bfloat16, values.shape), codes=(codes, torch.int8, values.shape),
-           scales=(scales, torch.float32, values.shape[:1]))
-    _check(_lib.relserve_quantise_rows_i8(_ptr(values), values.shape[0], values.shape[1], _ptr(codes), _ptr(scales), _stream(stream)),
+    rows, n = shape = values.shape
+    _dense("relserve_quantise_rows_i8", ("values", values, torch.bfloat16, shape), ("codes", codes, torch.int8, shape),
+           ("scales", scales, torch.float32, (rows,)))
+    _check(_lib.relserve_quantise_rows_i8(values.data_ptr(), rows, n, codes.data_ptr(), scales.data_ptr(), _stream_address(values, stream)),
            "relserve_quantise_rows_i8")
 
 
 def relserve_add_rmsnorm_i8(x, w, eps: float, codes, scales, delta=None, sum_out=None, stream=None) -> None:
     """codes [T, H] int8, scales [T] fp32 of the normed x + delta (x bf16 or fp32, delta bf16); sum_out (may be x): x + delta."""
-    f32 = x.dtype == torch.float32
-    _dense("relserve_add_rmsnorm_i8", x=(x, torch.float32 if f32 else torch.bfloat16, x.shape), w=(w, torch.bfloat16, x.shape[1:]),
-           codes=(codes, torch.int8, x.shape), scales=(scales, torch.float32, x.shape[:1]), delta=(delta, torch.bfloat16, x.shape),
-           sum_out=(sum_out, x.dtype, x.shape))
-    _check(_lib.relserve_add_rmsnorm_i8(_ptr(x), int(f32), _ptr(delta), _ptr(w), float(eps), x.shape[0], x.shape[1], _ptr(sum_out),
-                                        _ptr(codes), _ptr(scales), _stream(stream)), "relserve_add_rmsnorm_i8")
+    rows, n = shape = x.shape
+    f32 = x.dtype is torch.float32
+    dtype = torch.float32 if f32 else torch.bfloat16
+    _dense("relserve_add_rmsnorm_i8", ("x", x, dtype, shape), ("w", w, torch.bfloat16, (n,)), ("codes", codes, torch.int8, shape),
+           ("scales", scales, torch.float32, (rows,)), ("delta", delta, torch.bfloat16, shape), ("sum_out", sum_out, dtype, shape))
+    _check(_lib.relserve_add_rmsnorm_i8(x.data_ptr(), f32, _address(delta), w.data_ptr(), eps, rows, n, _address(sum_out), codes.data_ptr(),
+                                        scales.data_ptr(), _stream_address(x, stream)), "relserve_add_rmsnorm_i8")
 
 
 def relserve_linear_i8_workspace_bytes(tokens: int, n: int) -> int:
@@ -439,15 +451,16 @@ def relserve_linear_i8_workspace_bytes(tokens: int, n: int) -> int:
 def relserve_linear_i8(a, a_scale, w, w_scale, epilogue: int, residual, out, n: int = 0, workspace=None, stream=None) -> None:
     """a [T, K], w [N, K] int8 codes (n > 0: w is packed by pack_codes and has n rows), a_scale [T], w_scale [N] fp32.
     workspace: uint8 tensor of relserve_linear_i8_workspace_bytes(T, N) bytes or more, or None."""
-    t, k = a.shape
-    rows = int(n) if n else w.shape[0]
-    _dense("relserve_linear_i8", a=(a, torch.int8, a.shape), a_scale=(a_scale, torch.float32, a.shape[:1]),
-           w=(w, torch.int8, ((rows + 255) // 256 * 256 * k,) if n else (rows, k)), w_scale=(w_scale, torch.float32, (rows,)),
-           out=(out, torch.float32 if epilogue == 1 else torch.bfloat16, (t, rows // 2 if epilogue == 3 else rows)),
-           residual=(residual, torch.bfloat16 if epilogue == 1 else torch.float32, (t, rows)))
-    _check(_lib.relserve_linear_i8(_ptr(a), _ptr(a_scale), _ptr(w), _ptr(w_scale), t, rows, k, int(epilogue), _ptr(residual), _ptr(out),
-                                   int(n > 0), _ptr(workspace), 0 if workspace is None else workspace.numel() * workspace.element_size(),
-                                   _stream(stream)), "relserve_linear_i8")
+    t, k = shape = a.shape
+    rows = n if n else w.shape[0]
+    _dense("relserve_linear_i8", ("a", a, torch.int8, shape), ("a_scale", a_scale, torch.float32, (t,)),
+           ("w", w, torch.int8, ((rows + 255) // 256 * 256 * k,) if n else (rows, k)), ("w_scale", w_scale, torch.float32, (rows,)),
+           ("out", out, torch.float32 if epilogue == 1 else torch.bfloat16, (t, rows // 2 if epilogue == 3 else rows)),
+           ("residual", residual, torch.bfloat16 if epilogue == 1 else torch.float32, (t, rows)),
+           ("workspace", workspace, torch.uint8, workspace.shape if workspace is not None else ()))
+    _check(_lib.relserve_linear_i8(a.data_ptr(), a_scale.data_ptr(), w.data_ptr(), w_scale.data_ptr(), t, rows, k, epilogue, _address(residual),
+                                   out.data_ptr(), n > 0, _address(workspace), 0 if workspace is None else workspace.numel(),
+                                   _stream_address(a, stream)), "relserve_linear_i8")
 
 
 def relserve_static_scratch_bytes() -> int:

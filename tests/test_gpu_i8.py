@@ -61,7 +61,7 @@ def _check_codes(codes, scales, values, scale_tol, code_tol, what):
 
 
 ROW_SIZES = [(1, 8), (5, 64), (300, 256), (37, 1000), (24, 2048), (9, 2056), (130, 5120), (1282, 5120), (7, 8192), (33, 13824), (3, 28672),
-             (2, 65544), (2049, 512), (4100, 136)]
+             (2, 65544), (2049, 512), (4100, 136), (1030, 1336), (1030, 2048), (60, 11000), (5, 20488)]
 
 
 @pytest.mark.parametrize("t,n", ROW_SIZES)
@@ -111,6 +111,34 @@ def test_add_rmsnorm(rs, t, n, f32, delta, kept):
     # codes: the products s w, 127 / m, their product, and m's own rounding.  The scale: at most n / 64 squares in one chain, a tree of the
     # rest, of which the root halves the error, the quotient, root and reciprocal, m, its product and the division by 127
     _check_codes(codes, scales, values, ((n / 64 + 16) / 2 + 7) * U, 4.04 * U, f"{t} x {n}")
+
+
+@pytest.mark.parametrize("t,n", [(8300, 5136), (2500, 28680)])
+def test_rows_of_more_than_the_caches_hold(rs, t, n):
+    """As above where the passes stream; 64 of the rows, and the others' codes by their range and the scale they have."""
+    print(f"[case] large rows {t} x {n}", flush=True)
+    g = _gen(9)
+    x, d = (_stream(g, t, n) * 0.7).to(torch.bfloat16), _randn(g, t, n).to(torch.bfloat16)
+    w = (1.0 + 0.1 * _randn(g, n)).to(torch.bfloat16)
+    some = torch.arange(0, t, t // 64, device="cuda")
+    full_c, codes = _with_guard(t, n, dtype=torch.int8, fill=77)
+    full_s, scales = _with_guard(t, dtype=torch.float32, fill=-3.0)
+    full_o, out = _with_guard(t, n, dtype=torch.bfloat16, fill=9.0)
+    rs.relserve_add_rmsnorm_i8(x, w, 1e-5, codes, scales, delta=d, sum_out=out)
+    torch.cuda.synchronize()
+    assert torch.equal(out, (x.float() + d.float()).to(torch.bfloat16))
+    s = out[some].double()
+    _check_codes(codes[some], scales[some], s * w.double() / torch.sqrt(s.square().mean(1, keepdim=True) + 1e-5), ((n / 64 + 16) / 2 + 7) * U,
+                 4.04 * U, f"{t} x {n}")
+    assert bool((codes.abs().amax(1) == 127).all())
+    x = torch.cat([x, x])
+    full_c, codes = _with_guard(2 * t, n, dtype=torch.int8, fill=77)
+    full_s, scales = _with_guard(2 * t, dtype=torch.float32, fill=-3.0)
+    rs.relserve_quantise_rows_i8(x, codes, scales)
+    torch.cuda.synchronize()
+    _check_codes(codes[some], scales[some], x[some].double(), 1.01 * U, 2.02 * U, f"{t} x {n}")
+    assert torch.equal(codes[:t], codes[t:]) and torch.equal(scales[:t], scales[t:]) and bool((codes.abs().amax(1) == 127).all())
+    assert _untouched(full_c, 2 * t, 77) and _untouched(full_s, 2 * t, -3.0) and _untouched(full_o, t, 9.0)
 
 
 def test_rows_out_of_the_ordinary(rs):
