@@ -785,7 +785,7 @@ __global__ void __launch_bounds__(64 * WGM * WGN) gemm_dma_kernel(GemmArgs p) {
     uint32_t a_lane[KSTEPS], w_lane[KSTEPS];
 #pragma unroll
     for (int ks = 0; ks < KSTEPS; ++ks) {
-        const int c = F8 ? 2 * g : 4 * ks + g;   // the lane's (first) chunk of a row
+        const int c = F8 ? (kInt8 ? g : 2 * g) : 4 * ks + g;   // the lane's (first) chunk of a row
         const uint32_t at = lds0 + fr * ROWB + ((c ^ swz) << 4);
         a_lane[ks] = at + wm * (BM / WGM) * ROWB;
         const int row = frag_row16<EPI>(fr);
@@ -811,7 +811,7 @@ __global__ void __launch_bounds__(64 * WGM * WGN) gemm_dma_kernel(GemmArgs p) {
     typedef const i32x4_t __attribute__((address_space(3))) * lds_chunk;
     auto read_frag = [&](uint32_t at, int dist) __attribute__((always_inline)) -> frag_t {
         if constexpr (F8) {
-            const i32x4_t lo = *(lds_chunk)(uintptr_t)(at + dist), hi = *(lds_chunk)(uintptr_t)((at ^ 16) + dist);
+            const i32x4_t lo = *(lds_chunk)(uintptr_t)(at + dist), hi = *(lds_chunk)(uintptr_t)((at ^ (kInt8 ? 64 : 16)) + dist);
             return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
         } else {
             return __builtin_bit_cast(bf16x8_t, *(lds_chunk)(uintptr_t)(at + dist));
@@ -844,6 +844,14 @@ __global__ void __launch_bounds__(64 * WGM * WGN) gemm_dma_kernel(GemmArgs p) {
             acc[tn][tm] = rows32(EPI) ? mfma_16x16x128_f8(af[buf][tm], wf[buf][tn], acc[tn][tm]) : mfma_16x16x128_f8(wf[buf][tn], af[buf][tm], acc[tn][tm]);
         else
             acc[tn][tm] = rows32(EPI) ? mfma_16x16x32(af[buf][tm], wf[buf][tn], acc[tn][tm]) : mfma_16x16x32(wf[buf][tn], af[buf][tm], acc[tn][tm]);
+    };
+    // one of the two products of 64 codes of a pair of fragments (QUARTERS)
+    auto int8_half = [&](int tn, int tm, auto upper) __attribute__((always_inline)) {
+        constexpr int o = decltype(upper)::value ? 4 : 0;
+        if constexpr (F8 && kInt8) {
+            const i32x4_t wv = __builtin_shufflevector(wf[0][tn], wf[0][tn], o, o + 1, o + 2, o + 3), av = __builtin_shufflevector(af[0][tm], af[0][tm], o, o + 1, o + 2, o + 3);
+            acc[tn][tm] = __builtin_amdgcn_mfma_i32_16x16x64_i8(rows32(EPI) ? av : wv, rows32(EPI) ? wv : av, acc[tn][tm], 0, 0, 0);
+        }
     };
     // Source of the refill in progress (set at a hand-over): the k slice's first byte in both operands and the
     // freed stages' LDS addresses, so that a load costs its own two instructions plus one scalar add.
@@ -938,18 +946,32 @@ __global__ void __launch_bounds__(64 * WGM * WGN) gemm_dma_kernel(GemmArgs p) {
 #pragma unroll
         for (int i = 0; i < 2 * NQ; ++i) {
             const int q = i / NQ, j = i % NQ, a_half = second == (q == 0) ? 1 - h : h;
-            slot(second ? 0 : 1, i, refill_a, refill_w, [&]() __attribute__((always_inline)) { mfma_one(0, ((second ? WH : 0) + j / AH) * TM + a_half * AH + j % AH); });
+            const int tn = (second ? WH : 0) + j / AH, tm = a_half * AH + j % AH;
             // behind every other product, or, on tiles of few products, evenly
             const bool rd_w = second == (q == 0);
             const int nf = rd_w ? WH : AH;
             const int f0 = 2 * nf <= NQ + 1 ? (j + 1) / 2 : j * nf / NQ, f1 = 2 * nf <= NQ + 1 ? j / 2 + 1 : (j + 1) * nf / NQ;
+            auto reads = [&]() __attribute__((always_inline)) {
 #pragma unroll
-            for (int f = f0; f < min(f1, nf); ++f) {
-                if (rd_w)
-                    read_w(src, second ? 0 : 1, f);
-                else
-                    read_a(src, 1 - h, f);
-            }
+                for (int f = f0; f < min(f1, nf); ++f) {
+                    if (rd_w)
+                        read_w(src, second ? 0 : 1, f);
+                    else
+                        read_a(src, 1 - h, f);
+                }
+                __builtin_amdgcn_sched_barrier(0);
+            };
+            slot(second ? 0 : 1, i, refill_a, refill_w, [&]() __attribute__((always_inline)) {
+                if constexpr (kInt8) {
+                    int8_half(tn, tm, std::false_type{});
+                    __builtin_amdgcn_sched_barrier(0);
+                    reads();
+                    int8_half(tn, tm, std::true_type{});
+                } else {
+                    mfma_one(0, tn * TM + tm);
+                }
+            });
+            if constexpr (!kInt8) reads();
             __builtin_amdgcn_sched_barrier(0);
         }
     };
