@@ -238,7 +238,8 @@ class Product:
 
 LINEAR_SIZES = [(1, 4, 128), (1, 5120, 5120), (3, 16, 256), (24, 15360, 1024), (31, 260, 384), (33, 1004, 1152), (64, 256, 5120),
                 (65, 512, 2048), (128, 5120, 13824), (129, 132, 640), (192, 1024, 4096), (200, 2048, 128), (256, 640, 2560), (257, 512, 5120),
-                (300, 1000, 512), (385, 7168, 2560), (640, 5120, 1024), (1282, 5120, 640), (1384, 1536, 1024), (2100, 1088, 128)]
+                (300, 1000, 512), (385, 7168, 2560), (640, 5120, 1024), (1282, 5120, 640), (1384, 1536, 1024), (2100, 1088, 128), (17, 5120, 13824), (8, 4096, 28672), (50, 12288, 4096), (70, 10240, 640),
+                (12, 20480, 5120)]
 
 
 @pytest.mark.parametrize("packed", [False, True], ids=["rowmajor", "packed"])
@@ -277,6 +278,21 @@ def test_every_tile_and_split_gives_the_same_bits(rs, tile, splits):
                 assert torch.equal(got, w)
     finally:
         rs.relserve_debug_force_gemm_plan()
+
+
+@pytest.mark.parametrize("t,n,k,e", [(1, 5120, 5120, 0), (16, 1004, 1280, 0), (24, 2056, 2048, 0), (32, 27648, 4096, 3), (33, 512, 384, 0), (64, 10240, 2048, 0),
+                                     (60, 5124, 4096, 0), (100, 6000, 128, 0), (200, 2816, 1152, 3), (900, 520, 640, 0), (2, 57344, 2048, 3)])
+def test_small_problems_give_the_tiled_kernels_bits(rs, t, n, k, e):
+    """A forced tile sends these to the kernels of larger problems."""
+    for packed in (False, True):
+        print(f"[case] linear i8 T={t} N={n} K={k} epilogue {e} packed={packed}", flush=True)
+        p = Product(rs, t, n, k, packed)
+        got = p.check(e)
+        try:
+            rs.relserve_debug_force_gemm_plan(4, 0)
+            assert torch.equal(got, p.check(e))
+        finally:
+            rs.relserve_debug_force_gemm_plan()
 
 
 @pytest.mark.parametrize("t", [1, 40, 300])
