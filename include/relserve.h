@@ -338,6 +338,35 @@ int32_t relserve_linear_i8(const void* a, const float* a_scale, const void* w, c
                            int32_t epilogue, const void* residual, void* out, int32_t packed, void* workspace, size_t workspace_bytes,
                            void* stream);
 
+/* relserve_qkv_rope_append on codes h [T, H] with scales h_scale [T] and w_qkv with row scales s_qkv; packed as in relserve_linear_i8;
+ * workspace as in relserve_linear_i8 (N = (n_q + 2 n_kv) d), or NULL.  hidden a multiple of 128. */
+int32_t relserve_qkv_rope_append_i8(const relserve_layer* layer, const relserve_batch* batch, const void* h, const float* h_scale,
+                                    const void* w_qkv, const float* s_qkv, void* q_out, relserve_kv_cache cache, int32_t packed,
+                                    void* workspace, size_t workspace_bytes, void* stream);
+
+/* The layer step on these projections, bit for bit the calls of its stages one after the other: relserve_add_rmsnorm_i8 of x,
+ * relserve_qkv_rope_append_i8, relserve_attention, relserve_quantise_rows_i8, relserve_linear_i8 (W_o, epilogue 1 on x),
+ * relserve_add_rmsnorm_i8 of the fp32 stream, relserve_linear_i8 (gate/up, epilogue 3), relserve_quantise_rows_i8, relserve_linear_i8 (down,
+ * epilogue 2).  Cache, ownership and errors as relserve_layer_step; workspace of relserve_workspace_bytes.
+ * Pointers are device memory: w_* int8 [out, in] row by row, or (packed != 0) packed as in relserve_linear_i8; s_* fp32 [out].
+ * hidden, n_q_heads * head_dim and mlp_dim have to be multiples of 128, at most 130944, and mlp_dim below 2 hidden + 4 n_q_heads head_dim
+ * (RELSERVE_ERR_BAD_ARGUMENT otherwise). */
+typedef struct {
+    const void* w_in_norm;     /* [H] bf16 */
+    const void* w_qkv;         /* [(n_q + 2 n_kv) d, H] codes */
+    const float* s_qkv;        /* [(n_q + 2 n_kv) d] */
+    const void* w_o;           /* [H, n_q d] */
+    const float* s_o;          /* [H] */
+    const void* w_post_norm;   /* [H] bf16 */
+    const void* w_gate_up;     /* [2 I, H], gate rows then up rows */
+    const float* s_gate_up;    /* [2 I] */
+    const void* w_down;        /* [H, I] */
+    const float* s_down;       /* [H] */
+    int32_t packed;
+} relserve_layer_weights_i8;
+int32_t relserve_layer_step_i8(const relserve_layer* layer, const relserve_batch* batch, const relserve_layer_weights_i8* weights,
+                               const void* x, void* y, relserve_kv_cache cache, void* workspace, size_t workspace_bytes, void* stream);
+
 /* out[T, N] = a[T, K] * w[N, K]^T (Eq. 3 and every other dense map), bf16 in,
  * fp32 accumulate.  epilogue: 0 = store bf16; 1 = add residual (bf16 [T, N],
  * or none when NULL) and store fp32; 2 = add residual (fp32 [T, N]) and store bf16; 3 = SwiGLU:

@@ -39,7 +39,8 @@ EXPORTS = ["relserve_version", "relserve_strerror", "relserve_config_validate", 
            "relserve_aba_decide", "relserve_starved_priority", "relserve_static_priority", "relserve_utok_estimate",
            "relserve_priority_reuse", "relserve_prefill_candidate",
            "relserve_layer_step_w8a8", "relserve_model_step_w8a8", "relserve_rmsnorm_codes", "relserve_quantise_bf16", "relserve_linear_w8a8",
-           "relserve_quantise_rows_i8", "relserve_add_rmsnorm_i8", "relserve_linear_i8", "relserve_linear_i8_workspace_bytes"]
+           "relserve_quantise_rows_i8", "relserve_add_rmsnorm_i8", "relserve_linear_i8", "relserve_linear_i8_workspace_bytes",
+           "relserve_qkv_rope_append_i8", "relserve_layer_step_i8"]
 
 
 class RelserveError(RuntimeError):
@@ -91,6 +92,11 @@ class LayerWeightsW8A8(C.Structure):
     _fields_ = ([(n, C.c_void_p) for n in ("w_in_norm", "w_qkv", "s_qkv", "w_o", "s_o", "w_post_norm", "w_gate_up", "s_gate_up",
                                             "w_down", "s_down")]
                 + [(n, C.c_float) for n in ("a_qkv", "a_o", "a_gate_up", "a_down")] + [("packed", C.c_int32)])
+
+
+class LayerWeightsI8(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("w_in_norm", "w_qkv", "s_qkv", "w_o", "s_o", "w_post_norm", "w_gate_up", "s_gate_up", "w_down",
+                                          "s_down")] + [("packed", C.c_int32)]
 
 
 class Model(C.Structure):
@@ -150,6 +156,9 @@ for _n, _a in {
     "relserve_linear_i8_workspace_bytes": [C.c_int32, C.c_int32, C.c_void_p],
     "relserve_linear_i8": [C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_int32, C.c_int32, C.c_int32, C.c_int32, C.c_void_p,
                            C.c_void_p, C.c_int32, C.c_void_p, C.c_size_t, C.c_void_p],
+    "relserve_qkv_rope_append_i8": [C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, KVCache, C.c_int32,
+                                    C.c_void_p, C.c_size_t, C.c_void_p],
+    "relserve_layer_step_i8": [C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, KVCache, C.c_void_p, C.c_size_t, C.c_void_p],
     "relserve_model_workspace_bytes": [C.c_void_p, C.c_int32, C.c_int32, C.c_void_p],
     "relserve_model_step": [C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_size_t,
                             C.c_void_p],
@@ -461,6 +470,53 @@ def relserve_linear_i8(a, a_scale, w, w_scale, epilogue: int, residual, out, n: 
     _check(_lib.relserve_linear_i8(a.data_ptr(), a_scale.data_ptr(), w.data_ptr(), w_scale.data_ptr(), t, rows, k, epilogue, _address(residual),
                                    out.data_ptr(), n > 0, _address(workspace), 0 if workspace is None else workspace.numel(),
                                    _stream_address(a, stream)), "relserve_linear_i8")
+
+
+def relserve_qkv_rope_append_i8(layer, pbatch, h, h_scale, w_qkv, s_qkv, q_out, k_pages, v_pages, packed: bool = False, workspace=None,
+                                stream=None) -> None:
+    """h [T, H], w_qkv [(n_q + 2 n_kv) d, H] int8 codes (packed: converted by pack_codes), h_scale [T], s_qkv fp32; q_out [T, n_q d] bf16."""
+    t, k = shape = h.shape
+    rows = s_qkv.shape[0]
+    _dense("relserve_qkv_rope_append_i8", ("h", h, torch.int8, (pbatch.T, layer.shape.hidden)), ("h_scale", h_scale, torch.float32, (t,)),
+           ("w_qkv", w_qkv, torch.int8, ((rows + 255) // 256 * 256 * k,) if packed else (rows, k)),
+           ("s_qkv", s_qkv, torch.float32, (layer.shape.qkv_dim,)), ("q_out", q_out, torch.bfloat16, (t, layer.shape.q_dim)),
+           ("workspace", workspace, torch.uint8, workspace.shape if workspace is not None else ()))
+    _check(_lib.relserve_qkv_rope_append_i8(layer.handle, pbatch.handle, h.data_ptr(), h_scale.data_ptr(), w_qkv.data_ptr(), s_qkv.data_ptr(),
+                                            q_out.data_ptr(), _cache(k_pages, v_pages), bool(packed), _address(workspace),
+                                            0 if workspace is None else workspace.numel(), _stream_address(h, stream)),
+           "relserve_qkv_rope_append_i8")
+
+
+def quantise_layer_weights_i8(weights: dict) -> dict:
+    """The weights of relserve_layer_step_i8 from a layer's 16-bit ones (row-major device tensors): every output row by
+    relserve_quantise_rows_i8."""
+    out = {n: weights[n] for n in ("w_in_norm", "w_post_norm")}
+    for name in MATRIX_NAMES:
+        w = weights[name]
+        out[name] = torch.empty(w.shape, dtype=torch.int8, device=w.device)
+        out["s_" + name[2:]] = torch.empty(w.shape[0], dtype=torch.float32, device=w.device)
+        relserve_quantise_rows_i8(w, out[name], out["s_" + name[2:]])
+    return out
+
+
+def _weights_i8(layer, w: dict) -> LayerWeightsI8:
+    """w: codes w_* (int8, or packed by pack_layer_weights_w8a8), row scales s_* (fp32), norm weights (bf16) as device tensors."""
+    s, packed = layer.shape, bool(w.get("packed", False))
+    sizes = {"qkv": (s.qkv_dim, s.hidden), "o": (s.hidden, s.q_dim), "gate_up": (2 * s.mlp_dim, s.hidden), "down": (s.hidden, s.mlp_dim)}
+    _dense("relserve_layer_step_i8", *((n, w[n], torch.bfloat16, (s.hidden,)) for n in ("w_in_norm", "w_post_norm")),
+           *(("w_" + n, w["w_" + n], torch.int8, ((r + 255) // 256 * 256 * k,) if packed else (r, k)) for n, (r, k) in sizes.items()),
+           *(("s_" + n, w["s_" + n], torch.float32, (r,)) for n, (r, _) in sizes.items()))
+    return LayerWeightsI8(*[w[n].data_ptr() for n, t in LayerWeightsI8._fields_ if t is C.c_void_p], packed)
+
+
+def relserve_layer_step_i8(layer, pbatch, weights: dict, x, y, k_pages, v_pages, workspace, stream=None) -> None:
+    """weights: as quantise_layer_weights_i8 makes them, or these packed by pack_layer_weights_w8a8."""
+    shape = (pbatch.T, layer.shape.hidden)
+    _dense("relserve_layer_step_i8", ("x", x, torch.bfloat16, shape), ("y", y, torch.bfloat16, shape))
+    wt = _weights_i8(layer, weights)
+    _check(_lib.relserve_layer_step_i8(layer.handle, pbatch.handle, C.byref(wt), x.data_ptr(), y.data_ptr(), _cache(k_pages, v_pages),
+                                       workspace.data_ptr(), workspace.numel() * workspace.element_size(), _stream_address(x, stream)),
+           "relserve_layer_step_i8")
 
 
 def relserve_static_scratch_bytes() -> int:
