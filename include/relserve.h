@@ -315,10 +315,10 @@ int32_t relserve_linear_w8a8(const void* a, const void* w, const float* w_scale,
  *     scale = m / 127, m = the row's largest magnitude;  code = the integer nearest to value * 127 / m (ties to even)
  * so codes lie in [-127, 127].  A row of zeros has scale 0 and codes of 0; one with a NaN or an infinity has a scale that is not finite
  * and codes of 0: whatever is computed from it is not finite either.
- * All pointers are device memory: rows of values and weights and the codes 16-byte aligned (RELSERVE_ERR_BAD_ARGUMENT otherwise).
+ * All pointers are device memory, 16-byte aligned but for the scales of tokens (RELSERVE_ERR_BAD_ARGUMENT otherwise).
  *
  * relserve_quantise_rows_i8: codes and scales of the rows of in [n_rows, n] bf16 (activations, or weights: rows are output channels).
- * n a multiple of 8.
+ * n a multiple of 8; n_rows at most 2^30 here and below (RELSERVE_ERR_TOO_LARGE).
  *
  * relserve_add_rmsnorm_i8: the norm in front of a projection, with the residual's addition ahead of it.  s = x + delta, rounded to x's
  * type (bf16, or fp32 when x_is_f32); delta bf16 or NULL (s = x).  sum, if not NULL, receives s; it may be x, and overlaps nothing else.

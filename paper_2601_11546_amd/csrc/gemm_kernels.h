@@ -1735,6 +1735,8 @@ bool skinny_applies(int T, int N, int K, const float* accum) {
 // floats) use the tail scratch.
 int split_rows(int T, int N, int K, bool has_accum) {
     if (!has_accum || T <= SKINNY_MAX_T || K % 64 || N % 4 || forced_cand() >= 0) return 0;
+    // (integers may change tiles: k up to 4096 codes is faster whole, 4096 x 4096 at T = 640 26.6 -> 25.5, at 1000 31.7 -> 27.0)
+    if (kInt8 && K <= 2048) return 0;
     const int tn = (N + 255) / 256;
     if (((T + 127) / 128) * tn <= 128) return 128;
     if (((T + 255) / 256) * tn <= 85 && K >= 8192) return 256;
@@ -1742,9 +1744,9 @@ int split_rows(int T, int N, int K, bool has_accum) {
 }
 
 // k too short to cut (below 512): one k range leaves the sums of whole tiles, and the fused epilogue the bits of the finish kernel
-// (on codes it rounds once less), a launch and a pass over the slab less.  Gate/up of the tiny layer (hidden 256) with its finish kernel at
+// (on floating point codes it rounds once less), a launch and a pass over the slab less.  Gate/up of the tiny layer (hidden 256) with its finish kernel at
 // T = 482 / 1308 / 1947 14.8 / 14.9 / 17.0 us, whole 5.1 / 5.8 / 6.4; W_o at 1947 13.6, 6.0.
-bool one_range(const GemmArgs& p, int bm) { return !p.f8 && choose_splits(p.T, p.N, p.K, bm) == 1; }
+bool one_range(const GemmArgs& p, int bm) { return (kInt8 || !p.f8) && choose_splits(p.T, p.N, p.K, bm) == 1; }
 
 template <int EPI>
 hipError_t launch_mid_split(GemmArgs p, int bm, hipStream_t s, NextNorm* next) {

@@ -210,27 +210,36 @@ hipError_t launch_rows(GemmArgs p, hipStream_t s) {
 
 // Which problems go this way, and on which tile.  Every workgroup loads its own activations beside its weights, so the time is a launch, two
 // round trips and that traffic; the tiled kernels share both operands between more rows and columns, and win where the traffic gets long.
-// us, tiled kernels -> this one (three sets of operands in turn):
+// us, tiled kernels -> this one (three sets of operands in turn; outputs x k):
 //   T = 1: 5120 x 5120 10.5 -> 6.7, 15360 x 5120 17.8 -> 13.3, 5120 x 13824 17.0 -> 12.4, SwiGLU 27648 x 5120 26.6 -> 24.5; T = 8: 8192 x 28672 42.6 -> 38.3
 //   T = 24: 5120 x 5120 12.3 -> 7.3, 15360 x 5120 19.9 -> 14.0, 5120 x 13824 19.1 -> 13.2; but 5120 x 27648 (283 MB) 30.5 -> 39.3, SwiGLU 57344 x 8192 76 -> 86
-//   T = 40: 5120 x 13824 19.9 -> 15.8; 56: 15360 x 5120 22.0 -> 16.7; 96: 5120 x 5120 15.3 -> 13.3; 128: 5120 x 2048 12.9 -> 8.4
-//   T = 333: 1004 x 1152 12.2 -> 5.0; 500: 2048 x 2048 15.9 -> 9.4; 2000: 2048 x 512 17.2 -> 12.2; but 128: 5120 x 5120 (157 MB) 17.2 -> 17 .. 20 and
-//   SwiGLU 2816 x 512 at 1500 (104 MB) 8.6 -> 11.8
-// Tiles: one or two fragments of tokens as they need; with four, slices two deep where a CU gets one workgroup, else one deep and three
+//   T = 40: 5120 x 13824 19.9 -> 15.8; 56: 15360 x 5120 22.0 -> 16.7
+//   T = 128: 15360 x 5120 27.6 -> 23.7, SwiGLU 11264 x 5120 27.2 -> 18.9, 8192 x 8192 24.3 -> 19.9; but 5120 x 13824 (354 MB) 25.4 -> 27.5;
+//   100: 10240 x 8192 (252 MB) 24.8 -> 27.7; 256: 5120 x 5120 23.7 -> 19.2; 400: 4096 x 4096 22.7 -> 18.2; 520 (two rounds of tiles) 24.6 -> 30.2
+//   T = 333: 1004 x 1152 12.2 -> 5.0; 500: 2048 x 2048 15.9 -> 9.4; 700: 2560 x 2560 21.5 -> 14.8; 2000: 2048 x 512 17.2 -> 12.2; but SwiGLU
+//   2816 x 512 at 1500 (104 MB) 8.6 -> 11.8
+// Tiles: as few fragments of tokens as they need up to 64 tokens.  With four, slices two deep where a CU gets one workgroup, else one deep and three
 // workgroups (2000 x 2048 x 512 20.7, 12.2); four fragments of features for long k where they still fill the chip (64 x 10240 x 5120 17.0, 13.8).
-enum { ROWS_NONE = 0, ROWS_16, ROWS_32, ROWS_64, ROWS_64_SHALLOW, ROWS_64_WIDE };
+// More tokens: those tiles while their traffic is short, else 128 tokens a tile, in one round.
+enum { ROWS_NONE = 0, ROWS_16, ROWS_32, ROWS_64, ROWS_64_SHALLOW, ROWS_64_WIDE, ROWS_128, ROWS_128_WIDE };
 int rows_tile(const GemmArgs& p, int epi) {
     if (forced_cand() >= 0) return ROWS_NONE;
-    const bool paired = epi == EPI_SWIGLU || epi == EPI_QKV_ROPE;
-    const int64_t cols = epi == EPI_SWIGLU ? 2 * (int64_t)p.n_half : p.N, k_bytes = 2 * (int64_t)p.K;
+    const bool paired = epi == EPI_SWIGLU || epi == EPI_QKV_ROPE, swiglu = epi == EPI_SWIGLU;
+    const int64_t cols = swiglu ? 2 * (int64_t)p.n_half : p.N, k_bytes = 2 * (int64_t)p.K;
     auto tiles = [&](int fn, int tm) { return (int64_t)((p.T + 16 * tm - 1) / (16 * tm)) * (paired ? (cols / 2 + 8 * fn - 1) / (8 * fn) : (cols + 16 * fn - 1) / (16 * fn)); };
     auto traffic_mb = [&](int fn, int tm) { return tiles(fn, tm) * 16 * (fn + tm) * k_bytes >> 20; };
-    const bool swiglu = epi == EPI_SWIGLU;
+    auto fills = [&](int fn, int tm) { return tiles(fn, tm) >= 150 && tiles(fn, tm) <= 256; };   // one round of workgroups, most CUs busy
+    auto by_64 = [&] { return tiles(2, 4) > 256 ? ROWS_64_SHALLOW : tiles(2, 4) > 128 ? ROWS_64 : ROWS_32; };
     if (p.T <= 16) return traffic_mb(2, 1) <= (swiglu ? 256 : 400) ? ROWS_16 : ROWS_NONE;
     if (p.T <= 32) return traffic_mb(2, 2) <= 200 ? ROWS_32 : ROWS_NONE;
-    if (k_bytes >= 4096 && tiles(4, 4) >= 160 && traffic_mb(4, 4) <= (p.T <= 64 ? 200 : 128)) return ROWS_64_WIDE;
-    if (traffic_mb(2, 4) > (p.T <= 64 ? 224 : swiglu ? 80 : 128)) return ROWS_NONE;
-    return tiles(2, 4) > 256 ? ROWS_64_SHALLOW : tiles(2, 4) > 128 ? ROWS_64 : ROWS_32;
+    if (p.T <= 64) {
+        if (k_bytes >= 4096 && tiles(4, 4) >= 160 && traffic_mb(4, 4) <= 200) return ROWS_64_WIDE;
+        return traffic_mb(2, 4) <= 224 ? by_64() : ROWS_NONE;
+    }
+    if (traffic_mb(2, 4) <= (swiglu ? 80 : 128)) return by_64();
+    if (k_bytes >= 2048 && fills(4, 8) && traffic_mb(4, 8) <= 240) return ROWS_128_WIDE;
+    if (k_bytes >= 2048 && fills(2, 8) && traffic_mb(2, 8) <= 340) return ROWS_128;
+    return ROWS_NONE;
 }
 
 // Weights that the last-level cache (256 MB) cannot hold beside others are read with the non-temporal hint: SwiGLU 27648 x 5120 (141 MB) 27.2 ->
@@ -247,6 +256,8 @@ hipError_t run_rows(const GemmArgs& p, hipStream_t s, int tile) {
         case ROWS_64: return launch_rows<EPI, D, 2, 4, 4, 2, false>(p, s);
         case ROWS_64_SHALLOW: return launch_rows<EPI, D, 2, 4, 4, 1, false>(p, s);
         case ROWS_64_WIDE: return launch_rows<EPI, D, 4, 4, 8, 1, false>(p, s);
+        case ROWS_128: return launch_rows<EPI, D, 2, 8, 4, 1, false>(p, s);
+        case ROWS_128_WIDE: return launch_rows<EPI, D, 4, 8, 4, 1, false>(p, s);
         default: return hipErrorInvalidValue;
     }
 }

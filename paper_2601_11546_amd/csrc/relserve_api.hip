@@ -667,6 +667,8 @@ static inline bool aligned16(std::initializer_list<const void*> pointers) {
     return true;
 }
 
+static constexpr int32_t kMaxRowCodes = 1 << 30;   // rows are counted in 32 bits, a few past the last one too
+
 // Sums of products of 8-bit integers stay inside 32 bits: 2^14 K < 2^31.
 static constexpr int32_t kMaxKInt8 = 131072 - 128;
 
@@ -1243,6 +1245,7 @@ int32_t relserve_linear_w8a8(const void* a, const void* w, const float* w_scale,
 int32_t relserve_quantise_rows_i8(const void* in, int32_t n_rows, int32_t n, void* codes, float* scales, void* stream) {
     drop_stale_hip_error();
     if (n_rows < 0 || n <= 0 || n % 8) return RELSERVE_ERR_BAD_ARGUMENT;
+    if (n_rows > kMaxRowCodes) return RELSERVE_ERR_TOO_LARGE;
     if (n_rows == 0) return RELSERVE_OK;
     if (!in || !codes || !scales) return RELSERVE_ERR_NULL_POINTER;
     if (!aligned16({in, codes})) return RELSERVE_ERR_BAD_ARGUMENT;
@@ -1255,6 +1258,7 @@ int32_t relserve_add_rmsnorm_i8(const void* x, int32_t x_is_f32, const void* del
                                 int32_t hidden, void* sum, void* codes, float* scales, void* stream) {
     drop_stale_hip_error();
     if (n_rows < 0 || hidden <= 0 || hidden % 8) return RELSERVE_ERR_BAD_ARGUMENT;
+    if (n_rows > kMaxRowCodes) return RELSERVE_ERR_TOO_LARGE;
     if (n_rows == 0) return RELSERVE_OK;
     if (!x || !w || !codes || !scales) return RELSERVE_ERR_NULL_POINTER;
     if (!aligned16({x, delta, w, sum, codes})) return RELSERVE_ERR_BAD_ARGUMENT;

@@ -281,7 +281,8 @@ def test_every_tile_and_split_gives_the_same_bits(rs, tile, splits):
 
 
 @pytest.mark.parametrize("t,n,k,e", [(1, 5120, 5120, 0), (16, 1004, 1280, 0), (24, 2056, 2048, 0), (32, 27648, 4096, 3), (33, 512, 384, 0), (64, 10240, 2048, 0),
-                                     (60, 5124, 4096, 0), (100, 6000, 128, 0), (200, 2816, 1152, 3), (900, 520, 640, 0), (2, 57344, 2048, 3)])
+                                     (60, 5124, 4096, 0), (100, 6000, 128, 0), (200, 2816, 1152, 3), (900, 520, 640, 0), (2, 57344, 2048, 3), (130, 10000, 2176, 0), (128, 11264, 5120, 3),
+                                     (75, 7172, 4096, 0), (250, 3600, 5120, 3), (640, 2560, 4096, 0)])
 def test_small_problems_give_the_tiled_kernels_bits(rs, t, n, k, e):
     """A forced tile sends these to the kernels of larger problems."""
     for packed in (False, True):

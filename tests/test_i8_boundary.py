@@ -35,6 +35,7 @@ def test_rows(rs):
     assert _quantise(rs, inp=ODD) == BAD and _quantise(rs, codes=ODD) == BAD
     assert _norm(rs, rows=-1) == BAD and _norm(rs, n=0) == BAD and _norm(rs, n=4) == BAD
     assert _norm(rs, rows=0, x=None) == 0
+    assert _quantise(rs, rows=(1 << 30) + 1) == TOO_LARGE and _norm(rs, rows=2147483647) == TOO_LARGE
     for name in ("x", "w", "codes", "scales"):
         assert _norm(rs, **{name: None}) == NULL
     for name in ("x", "w", "codes", "delta", "total"):
