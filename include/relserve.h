@@ -282,6 +282,14 @@ int32_t relserve_model_step_w8a8(const relserve_layer* layer, const relserve_bat
                                  const int32_t* token_ids, void* logits,
                                  void* workspace, size_t workspace_bytes, void* stream);
 
+/* relserve_model_step with the int8 projections of relserve_layer_step_i8 (below) in every layer: `layers` is a HOST array of
+ * model->n_layers entries (model->layers is not read); everything else as in relserve_model_step. */
+struct relserve_layer_weights_i8;
+int32_t relserve_model_step_i8(const relserve_layer* layer, const relserve_batch* batch,
+                               const relserve_model* model, const struct relserve_layer_weights_i8* layers,
+                               const int32_t* token_ids, void* logits,
+                               void* workspace, size_t workspace_bytes, void* stream);
+
 /* Greedy decoding after the output layer (Sec. 2.3 "LLM Inference": the output layer's result for a
  * request's last token determines its next token): next_token[r] = the vocabulary entry with the largest
  * logit of row r, the lowest id among equal largest ones; NaN entries never win, a row without any number
@@ -351,7 +359,7 @@ int32_t relserve_qkv_rope_append_i8(const relserve_layer* layer, const relserve_
  * Pointers are device memory: w_* int8 [out, in] row by row, or (packed != 0) packed as in relserve_linear_i8; s_* fp32 [out].
  * hidden, n_q_heads * head_dim and mlp_dim have to be multiples of 128, at most 130944, and mlp_dim below 2 hidden + 4 n_q_heads head_dim
  * (RELSERVE_ERR_BAD_ARGUMENT otherwise). */
-typedef struct {
+typedef struct relserve_layer_weights_i8 {
     const void* w_in_norm;     /* [H] bf16 */
     const void* w_qkv;         /* [(n_q + 2 n_kv) d, H] codes */
     const float* s_qkv;        /* [(n_q + 2 n_kv) d] */

@@ -40,7 +40,7 @@ EXPORTS = ["relserve_version", "relserve_strerror", "relserve_config_validate", 
            "relserve_priority_reuse", "relserve_prefill_candidate",
            "relserve_layer_step_w8a8", "relserve_model_step_w8a8", "relserve_rmsnorm_codes", "relserve_quantise_bf16", "relserve_linear_w8a8",
            "relserve_quantise_rows_i8", "relserve_add_rmsnorm_i8", "relserve_linear_i8", "relserve_linear_i8_workspace_bytes",
-           "relserve_qkv_rope_append_i8", "relserve_layer_step_i8"]
+           "relserve_qkv_rope_append_i8", "relserve_layer_step_i8", "relserve_model_step_i8"]
 
 
 class RelserveError(RuntimeError):
@@ -164,6 +164,7 @@ for _n, _a in {
                             C.c_void_p],
     "relserve_model_step_w8a8": [C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_size_t,
                                  C.c_void_p],
+    "relserve_model_step_i8": [C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p],
     "relserve_greedy_sample": [C.c_void_p, C.c_int32, C.c_int32, C.c_void_p, C.c_void_p],
     "relserve_rmsnorm": [C.c_void_p, C.c_int32, C.c_void_p, C.c_float, C.c_int32, C.c_int32, C.c_void_p, C.c_void_p],
     "relserve_linear": [C.c_void_p, C.c_void_p, C.c_int32, C.c_int32, C.c_int32, C.c_int32, C.c_void_p,
@@ -534,10 +535,20 @@ def relserve_model_workspace_bytes(layer: Layer, max_tokens: int, max_reqs: int)
 
 def relserve_model_step(layer, pbatch, model: dict, token_ids, logits, workspace, stream=None) -> None:
     """model = {"embedding", "layers": [weights dict], "caches": [(k_pages, v_pages)], "w_final_norm", "w_lm_head"}
-    of torch tensors.  Layers whose dicts carry row scales ("s_qkv") run with quantised projections."""
+    of torch tensors.  Layers whose dicts carry row scales ("s_qkv") run with quantised projections: 8-bit floating point codes where they
+    carry input scales too ("a_qkv"), else integers."""
     n = len(model["layers"])
     w8a8 = n > 0 and "s_qkv" in model["layers"][0]
+    int8 = w8a8 and "a_qkv" not in model["layers"][0]
     lc = (KVCache * n)(*[_cache(k, v) for k, v in model["caches"]])
+    if int8:
+        lw = (LayerWeightsI8 * n)(*[_weights_i8(layer, w) for w in model["layers"]])
+        m = Model(n, model["embedding"].shape[0], model["embedding"].data_ptr(), None,
+                  C.cast(lc, C.c_void_p), model["w_final_norm"].data_ptr(), model["w_lm_head"].data_ptr())
+        _check(_lib.relserve_model_step_i8(layer.handle, pbatch.handle, C.byref(m), C.cast(lw, C.c_void_p), _ptr(token_ids),
+                                           _ptr(logits), _ptr(workspace), workspace.numel() * workspace.element_size(),
+                                           _stream(stream)), "relserve_model_step_i8")
+        return
     if w8a8:
         lw = (LayerWeightsW8A8 * n)(*[_weights_w8a8(w) for w in model["layers"]])
         m = Model(n, model["embedding"].shape[0], model["embedding"].data_ptr(), None,

@@ -676,6 +676,8 @@ __device__ __forceinline__ void dma16(const void* base, uint32_t voff, uint32_t 
 // F8: both operands hold 8-bit codes.  Nothing changes in how bytes travel (K counts pairs of codes, a stage row is
 // still 128 bytes); a stage is one k step of 16 x 16 x 128 MFMAs, whose operand is the two adjacent 16-byte chunks
 // 2 g, 2 g + 1 of the row for k quarter g (both operands alike, so which codes meet which is fixed), and the epilogue applies the scales.
+// (Of integers it is two steps of 16 x 16 x 64, on chunks g and g + 4: sixteen lanes then read all banks once, where adjacent chunks meet in
+// pairs.  Exact sums let the codes meet in any order.  8192 x 27648 x 5120 815 -> 798 us, SQ_LDS_BANK_CONFLICT 7.2e7 -> 0.)
 // NSW = stages of the weights' ring: NS, or NS + 1 ("skewed").  Loads of one wave complete in order, so a hand-over of the
 // skewed ring issues the activations of stage kt + NS first and the weights of stage kt + NS + 1 behind them: what the next
 // hand-over waits for are the activations, and the weights just issued stay in flight for another iteration.
@@ -940,6 +942,8 @@ __global__ void __launch_bounds__(64 * WGM * WGN) gemm_dma_kernel(GemmArgs p) {
     constexpr int WH = TN / 2, AH = TM / 2, NQ = WH * AH;
     auto read_w = [&](Source src, int half, int i) __attribute__((always_inline)) { wf[0][half * WH + i] = read_frag(src.w, w_dist(half * WH + i)); };
     auto read_a = [&](Source src, int half, int i) __attribute__((always_inline)) { af[0][half * AH + i] = read_frag(src.a, a_dist(half * AH + i)); };
+    // (Integers: the reads stand between a pair's two products of half the length.  All first halves of two pairs ahead of their second ones do
+    // not help: the compiler then moves the sums between the register files, 1630 us for 800.)
     auto half_step = [&](bool second, int h, Stage rd_stage, auto refill_a, auto refill_w) __attribute__((always_inline)) {
         const Source src = source(rd_stage, 0);
         __builtin_amdgcn_sched_barrier(0);
@@ -1821,14 +1825,13 @@ hipError_t launch_cfg(const GemmArgs& base, hipStream_t s, const Plan& plan = Pl
     constexpr int dma_smem = (DMA_NS * BM + DMA_NSW * BN) * DMA_BK * 2;
     const int tiles = p.tiles_m * p.tiles_n;
     if (p.K % 64 != 0) {
-        if constexpr (kInt8) return hipErrorInvalidValue;
-        if (p.f8) return hipErrorInvalidValue;   // codes go through the direct-to-LDS kernel only
+        if (kInt8 || p.f8) return hipErrorInvalidValue;   // codes go through the direct-to-LDS kernel only
         if constexpr (!kInt8) {
-        static std::once_flag once_generic;
-        static hipError_t st_generic = hipSuccess;
-        if (hipError_t e = allow_smem_once(once_generic, st_generic, &gemm_bf16_kernel<BM, BN, EPI, D>, smem)) return e;
-        gemm_bf16_kernel<BM, BN, EPI, D><<<dim3(tiles), dim3(256), smem, s>>>(p);
-        return hipGetLastError();
+            static std::once_flag once_generic;
+            static hipError_t st_generic = hipSuccess;
+            if (hipError_t e = allow_smem_once(once_generic, st_generic, &gemm_bf16_kernel<BM, BN, EPI, D>, smem)) return e;
+            gemm_bf16_kernel<BM, BN, EPI, D><<<dim3(tiles), dim3(256), smem, s>>>(p);
+            return hipGetLastError();
         }
     }
     int grid = tiles;

@@ -3,62 +3,18 @@
 #include <algorithm>
 #include <cmath>
 #include <cstring>
-#include <initializer_list>
 #include <mutex>
 #include <new>
 
-#include "relserve_internal.h"
+#include "relserve_host.h"
 
 using namespace relserve;
 
 namespace {
 
-constexpr size_t kAlign = 256;
-inline size_t align_up(size_t v) { return (v + kAlign - 1) / kAlign * kAlign; }
-
 const char* const kSlotNames[RELSERVE_PROFILE_SLOTS] = {
     "rmsnorm_in", "gemm_qkv_rope_append", "attn_own_keys", "attn_prefix", "attn_tile", "attn_split",
     "gemm_o",     "rmsnorm_post", "gemm_gate_up", "gemm_down",  "attn_merge", "quantise_attn"};
-// the last slot is the int8 step's (its other pass over rows counts with the down projection); the attention kernels store the codes of
-// relserve_layer_step_w8a8 themselves
-enum { S_NORM1 = 0, S_QKV, S_ATTN_OWN, S_ATTN_PREFIX, S_ATTN_TILE, S_ATTN_SPLIT, S_O, S_NORM2, S_GU, S_DOWN, S_ATTN_MERGE, S_QUANTISE };
-
-struct Workspace {
-    char* h;         // [T, H] bf16 (normed activations; reused for the post norm)
-    char* q;         // [T, q_dim] bf16 rotated queries
-    char* attn;      // [T, q_dim] bf16
-    char* x1;        // [T, H] fp32 residual stream after attention
-    char* act;       // [T, I] bf16
-    float* part_o;   // [T + split slots, n_q, d] fp32
-    float* part_ml;  // [T + split slots, n_q, 2] fp32
-    float* accum;    // fp32 split-K scratch of the GEMMs
-    size_t accum_floats;
-    size_t total;
-};
-
-Workspace carve(const relserve_layer& L, int64_t T, void* base) {
-    Workspace w;
-    size_t off = 0;
-    auto take = [&](size_t bytes) {
-        char* p = base ? static_cast<char*>(base) + off : nullptr;
-        off += align_up(bytes);
-        return p;
-    };
-    const relserve_layer_config& c = L.cfg;
-    w.h = take((size_t)T * c.hidden * 2);
-    w.q = take((size_t)T * L.q_dim * 2);
-    w.attn = take((size_t)T * L.q_dim * 2);
-    w.x1 = take((size_t)T * c.hidden * 4);
-    w.act = take((size_t)T * c.mlp_dim * 2);
-    const size_t part_rows = (size_t)(T + split_slot_cap(T));
-    w.part_o = reinterpret_cast<float*>(take(part_rows * L.q_dim * 4));
-    w.part_ml = reinterpret_cast<float*>(take(part_rows * c.n_q_heads * 2 * 4));
-    w.accum_floats = (size_t)gemm_scratch_floats(T, std::max({L.qkv_dim, 2 * c.mlp_dim, c.hidden}));
-    w.accum = reinterpret_cast<float*>(take(w.accum_floats * 4));
-    w.total = off;
-    return w;
-}
-
 // Cut of a batch of decode rows (see expand_batch): per shared prefix the number and length of its chunks, and the length
 // of the chunks of own keys.
 struct SlotPlan {
@@ -121,21 +77,6 @@ SlotPlan plan_slots(const relserve_layer_config& cfg, const relserve_batch_desc&
     return plan;
 }
 
-// Where the attention passes of a batch keep partial state: the workspace's own rows, or (slot plans) the GEMM scratch.
-struct PartialState { float* o; float* ml; };
-PartialState partial_state(const relserve_layer& L, const BatchDev& b, const Workspace& w) {
-    if (b.n_scratch_slots == 0) return {w.part_o, w.part_ml};
-    return {w.accum, w.accum + (int64_t)b.n_scratch_slots * L.q_dim};
-}
-
-// The cut of the attention a step over these pools runs.  A 16-bit output that rounds the other way moves codes of the keys and
-// values the next layer appends to its quantised pool, and those move the rest of the stack (3 % of the codes of a third 13B
-// layer, 2e-2 of the logits after four), so over quantised pools every entry point takes the cut without slots, whose results
-// stacks were recorded with.
-const BatchDev& attention_batch(const relserve_batch& b, const relserve_kv_cache& cache) {
-    return cache.dtype == RELSERVE_KV_FP8 ? b.dev_no_slots : b.dev;
-}
-
 bool is_pow2(int32_t v) { return v > 0 && (v & (v - 1)) == 0; }
 
 // Workspace of relserve_layer_step_static: a fixed array in device memory, one copy per GPU the library runs on,
@@ -158,33 +99,6 @@ int32_t static_scratch(void** out) {
         g_scratch_ptr[dev] = ptr;
     }
     *out = g_scratch_ptr[dev];
-    return RELSERVE_OK;
-}
-
-KvFormat kv_format(const relserve_kv_cache& cache) {
-    KvFormat f;
-    f.fp8 = cache.dtype == RELSERVE_KV_FP8;
-    if (f.fp8) f.k_scale = cache.k_scale, f.v_scale = cache.v_scale;
-    return f;
-}
-
-int32_t check_cache(const relserve_batch* b, const relserve_kv_cache& cache, bool fp8_ok = true) {
-    if (!cache.k_pages || !cache.v_pages) return RELSERVE_ERR_NULL_POINTER;
-    if (cache.dtype != RELSERVE_KV_BF16 && cache.dtype != RELSERVE_KV_FP8) return RELSERVE_ERR_BAD_ARGUMENT;
-    if (cache.dtype == RELSERVE_KV_FP8) {
-        if (!fp8_ok) return RELSERVE_ERR_BAD_ARGUMENT;
-        if (!(cache.k_scale > 0.0f) || !(cache.v_scale > 0.0f) || !std::isfinite(cache.k_scale) || !std::isfinite(cache.v_scale))
-            return RELSERVE_ERR_BAD_ARGUMENT;
-    }
-    if (cache.num_pages < b->dev.num_pages) return RELSERVE_ERR_MISMATCH;
-    return RELSERVE_OK;
-}
-
-// stream: where the caller submits work that reads the batch
-int32_t check_pair(const relserve_layer* L, const relserve_batch* b, const void* stream) {
-    if (!L || !b) return RELSERVE_ERR_NULL_POINTER;
-    if (std::memcmp(&L->cfg, &b->cfg, sizeof(relserve_layer_config)) != 0) return RELSERVE_ERR_MISMATCH;
-    if (stream) b->other_stream.store(true, std::memory_order_relaxed);
     return RELSERVE_OK;
 }
 
@@ -656,22 +570,6 @@ int32_t relserve::expand_batch(const relserve_layer_config& cfg, const relserve_
 // ------------------------------------------------------------------------------------------
 // plain entry points
 // ------------------------------------------------------------------------------------------
-// The launchers report hipGetLastError() after a launch; an error an earlier, unrelated HIP call of this thread left
-// behind (the runtime keeps the last one until it is read) must not be taken for theirs.
-static inline void drop_stale_hip_error() { (void)hipGetLastError(); }
-
-// Operands that kernels read and write 16 bytes at a time (null: not given).
-static inline bool aligned16(std::initializer_list<const void*> pointers) {
-    for (const void* p : pointers)
-        if (reinterpret_cast<uintptr_t>(p) % 16) return false;
-    return true;
-}
-
-static constexpr int32_t kMaxRowCodes = 1 << 30;   // rows are counted in 32 bits, a few past the last one too
-
-// Sums of products of 8-bit integers stay inside 32 bits: 2^14 K < 2^31.
-static constexpr int32_t kMaxKInt8 = 131072 - 128;
-
 extern "C" {
 
 int32_t relserve_version(void) { return 100; }
@@ -1130,67 +1028,6 @@ int32_t layer_step_codes(const relserve_layer* L, const relserve_batch* b, const
     run(S_DOWN, [&] { return launch_linear(w.act, wt->w_down, T, c.hidden, c.mlp_dim, 2, w.x1, y, s, accum, packed, &down); });
     return e == hipSuccess ? RELSERVE_OK : RELSERVE_ERR_HIP;
 }
-
-// Codes [T, n] and, behind them, their scales [T] in a buffer of the workspace (n is a multiple of 128).
-float* scales_behind(char* codes, int64_t T, int64_t n) { return reinterpret_cast<float*>(codes + T * n); }
-
-int32_t layer_step_int8(const relserve_layer* L, const relserve_batch* b, const relserve_layer_weights_i8* wt, const void* x, void* y,
-                        relserve_kv_cache cache, void* workspace, size_t workspace_bytes, void* stream) {
-    if (int32_t rc = check_pair(L, b, stream)) return rc;
-    if (!wt) return RELSERVE_ERR_NULL_POINTER;
-    if (int32_t rc = check_cache(b, cache)) return rc;
-    const relserve_layer_config& c = L->cfg;
-    for (int64_t k : {(int64_t)c.hidden, (int64_t)L->q_dim, (int64_t)c.mlp_dim})
-        if (k % 128 || k > kMaxKInt8) return RELSERVE_ERR_BAD_ARGUMENT;
-    if ((int64_t)c.mlp_dim >= 2 * (int64_t)c.hidden + 4 * (int64_t)L->q_dim) return RELSERVE_ERR_BAD_ARGUMENT;   // see `act` below
-    const int32_t T = b->dev.T;
-    if (T == 0) return RELSERVE_OK;
-    if (!x || !y || !wt->w_in_norm || !wt->w_qkv || !wt->w_o || !wt->w_post_norm || !wt->w_gate_up || !wt->w_down ||
-        !wt->s_qkv || !wt->s_o || !wt->s_gate_up || !wt->s_down)
-        return RELSERVE_ERR_NULL_POINTER;
-    if (!aligned16({x, y, wt->w_in_norm, wt->w_qkv, wt->w_o, wt->w_post_norm, wt->w_gate_up, wt->w_down, wt->s_qkv, wt->s_o, wt->s_gate_up, wt->s_down}))
-        return RELSERVE_ERR_BAD_ARGUMENT;
-    const bool packed = wt->packed != 0;
-    const int64_t widest = std::max({c.hidden, L->q_dim, c.mlp_dim});
-    auto matrix = [&](int64_t rows, int64_t k) { return (packed ? (rows + 255) / 256 * 256 : rows) * k; };
-    if (T * widest >= ((int64_t)1 << 31) || std::max({matrix(L->qkv_dim, c.hidden), matrix(c.hidden, L->q_dim), matrix(2 * (int64_t)c.mlp_dim, c.hidden),
-                                                      matrix(c.hidden, c.mlp_dim)}) >= ((int64_t)1 << 31))
-        return RELSERVE_ERR_TOO_LARGE;
-    if (!workspace || (reinterpret_cast<uintptr_t>(workspace) % kAlign)) return RELSERVE_ERR_WORKSPACE;
-    Workspace w = carve(*L, T, workspace);
-    if (w.total > workspace_bytes) return RELSERVE_ERR_WORKSPACE;
-    hipStream_t s = static_cast<hipStream_t>(stream);
-    relserve_layer* prof = L->profile ? const_cast<relserve_layer*>(L) : nullptr;
-    hipError_t e = hipSuccess;
-    auto run = [&](int slot, auto&& launch) {
-        if (e != hipSuccess) return;
-        profile_mark(prof, slot, s, true);
-        e = launch();
-        profile_mark(prof, slot, s, false);
-    };
-    // Codes live where the 16-bit step keeps what is over by then: of the norms in h, of the attention in q, of the SwiGLU product from h on
-    // through q and attn (2 T H + 4 T q_dim bytes).
-    char *h = w.h, *attn = w.q, *act = w.h;
-    float *h_s = scales_behind(h, T, c.hidden), *attn_s = scales_behind(attn, T, L->q_dim), *act_s = scales_behind(act, T, c.mlp_dim);
-    const BatchDev& batch = attention_batch(*b, cache);
-    const PartialState part = partial_state(*L, batch, w);
-    const KvFormat kv = kv_format(cache);
-    run(S_NORM1, [&] { return launch_row_codes(x, false, nullptr, wt->w_in_norm, c.rms_eps, T, c.hidden, nullptr, h, h_s, s); });
-    run(S_QKV, [&] {
-        return launch_qkv_rope_append_i8(b->dev, *L, h, h_s, wt->w_qkv, wt->s_qkv, w.q, cache.k_pages, cache.v_pages, s, w.accum, packed, kv);
-    });
-    if (e == hipSuccess)
-        e = launch_attention(batch, *L, w.q, L->q_dim, cache.k_pages, cache.v_pages, w.attn, part.o, part.ml, s, prof, kv);
-    run(S_QUANTISE, [&] { return launch_row_codes(w.attn, false, nullptr, nullptr, 0.0f, T, L->q_dim, nullptr, attn, attn_s, s); });
-    run(S_O, [&] { return launch_linear_i8(attn, attn_s, wt->w_o, wt->s_o, T, c.hidden, L->q_dim, 1, x, w.x1, s, w.accum, packed); });
-    run(S_NORM2, [&] { return launch_row_codes(w.x1, true, nullptr, wt->w_post_norm, c.rms_eps, T, c.hidden, nullptr, h, h_s, s); });
-    run(S_GU, [&] { return launch_linear_i8(h, h_s, wt->w_gate_up, wt->s_gate_up, T, 2 * c.mlp_dim, c.hidden, 3, nullptr, w.act, s, w.accum, packed); });
-    run(S_DOWN, [&] {
-        const hipError_t q = launch_row_codes(w.act, false, nullptr, nullptr, 0.0f, T, c.mlp_dim, nullptr, act, act_s, s);
-        return q != hipSuccess ? q : launch_linear_i8(act, act_s, wt->w_down, wt->s_down, T, c.hidden, c.mlp_dim, 2, w.x1, y, s, w.accum, packed);
-    });
-    return e == hipSuccess ? RELSERVE_OK : RELSERVE_ERR_HIP;
-}
 }  // namespace
 
 int32_t relserve_layer_step(const relserve_layer* L, const relserve_batch* b, const relserve_layer_weights* wt,
@@ -1242,85 +1079,6 @@ int32_t relserve_linear_w8a8(const void* a, const void* w, const float* w_scale,
     return e == hipSuccess ? RELSERVE_OK : RELSERVE_ERR_HIP;
 }
 
-int32_t relserve_quantise_rows_i8(const void* in, int32_t n_rows, int32_t n, void* codes, float* scales, void* stream) {
-    drop_stale_hip_error();
-    if (n_rows < 0 || n <= 0 || n % 8) return RELSERVE_ERR_BAD_ARGUMENT;
-    if (n_rows > kMaxRowCodes) return RELSERVE_ERR_TOO_LARGE;
-    if (n_rows == 0) return RELSERVE_OK;
-    if (!in || !codes || !scales) return RELSERVE_ERR_NULL_POINTER;
-    if (!aligned16({in, codes})) return RELSERVE_ERR_BAD_ARGUMENT;
-    return launch_row_codes(in, false, nullptr, nullptr, 0.0f, n_rows, n, nullptr, codes, scales, static_cast<hipStream_t>(stream)) == hipSuccess
-               ? RELSERVE_OK
-               : RELSERVE_ERR_HIP;
-}
-
-int32_t relserve_add_rmsnorm_i8(const void* x, int32_t x_is_f32, const void* delta, const void* w, float eps, int32_t n_rows,
-                                int32_t hidden, void* sum, void* codes, float* scales, void* stream) {
-    drop_stale_hip_error();
-    if (n_rows < 0 || hidden <= 0 || hidden % 8) return RELSERVE_ERR_BAD_ARGUMENT;
-    if (n_rows > kMaxRowCodes) return RELSERVE_ERR_TOO_LARGE;
-    if (n_rows == 0) return RELSERVE_OK;
-    if (!x || !w || !codes || !scales) return RELSERVE_ERR_NULL_POINTER;
-    if (!aligned16({x, delta, w, sum, codes})) return RELSERVE_ERR_BAD_ARGUMENT;
-    return launch_row_codes(x, x_is_f32 != 0, delta, w, eps, n_rows, hidden, sum, codes, scales, static_cast<hipStream_t>(stream)) == hipSuccess
-               ? RELSERVE_OK
-               : RELSERVE_ERR_HIP;
-}
-
-int32_t relserve_linear_i8_workspace_bytes(int32_t T, int32_t N, size_t* out) {
-    if (!out) return RELSERVE_ERR_NULL_POINTER;
-    if (T < 0 || N <= 0) return RELSERVE_ERR_BAD_ARGUMENT;
-    *out = (size_t)gemm_scratch_floats(T, N) * 4;
-    return RELSERVE_OK;
-}
-
-int32_t relserve_linear_i8(const void* a, const float* a_scale, const void* w, const float* w_scale, int32_t T, int32_t N, int32_t K,
-                           int32_t epilogue, const void* residual, void* out, int32_t packed, void* workspace, size_t workspace_bytes,
-                           void* stream) {
-    drop_stale_hip_error();
-    if (T < 0 || N <= 0 || K <= 0 || K % 128 || epilogue < 0 || epilogue > 3) return RELSERVE_ERR_BAD_ARGUMENT;
-    if (epilogue == 3 ? N % 16 : N % 4) return RELSERVE_ERR_BAD_ARGUMENT;
-    const int64_t w_rows = packed ? ((int64_t)N + 255) / 256 * 256 : N;
-    if (K > kMaxKInt8 || (int64_t)T * K >= ((int64_t)1 << 31) || w_rows * K >= ((int64_t)1 << 31)) return RELSERVE_ERR_TOO_LARGE;
-    if (T == 0) return RELSERVE_OK;
-    if (!a || !a_scale || !w || !w_scale || !out) return RELSERVE_ERR_NULL_POINTER;
-    if (epilogue == 2 && !residual) return RELSERVE_ERR_NULL_POINTER;
-    if (!aligned16({a, w, w_scale, residual, out})) return RELSERVE_ERR_BAD_ARGUMENT;
-    if (workspace && (reinterpret_cast<uintptr_t>(workspace) % kAlign || workspace_bytes < (size_t)gemm_scratch_floats(T, N) * 4))
-        return RELSERVE_ERR_WORKSPACE;
-    return launch_linear_i8(a, a_scale, w, w_scale, T, N, K, epilogue, residual, out, static_cast<hipStream_t>(stream),
-                            static_cast<float*>(workspace), packed != 0) == hipSuccess
-               ? RELSERVE_OK
-               : RELSERVE_ERR_HIP;
-}
-
-int32_t relserve_qkv_rope_append_i8(const relserve_layer* L, const relserve_batch* b, const void* h, const float* h_scale,
-                                    const void* w_qkv, const float* s_qkv, void* q_out, relserve_kv_cache cache, int32_t packed,
-                                    void* workspace, size_t workspace_bytes, void* stream) {
-    drop_stale_hip_error();
-    if (int32_t rc = check_pair(L, b, stream)) return rc;
-    if (int32_t rc = check_cache(b, cache)) return rc;
-    const int32_t T = b->dev.T, H = L->cfg.hidden;
-    if (H % 128) return RELSERVE_ERR_BAD_ARGUMENT;
-    const int64_t w_rows = packed ? ((int64_t)L->qkv_dim + 255) / 256 * 256 : L->qkv_dim;
-    if (H > kMaxKInt8 || (int64_t)T * H >= ((int64_t)1 << 31) || w_rows * H >= ((int64_t)1 << 31)) return RELSERVE_ERR_TOO_LARGE;
-    if (T == 0) return RELSERVE_OK;
-    if (!h || !h_scale || !w_qkv || !s_qkv || !q_out) return RELSERVE_ERR_NULL_POINTER;
-    if (!aligned16({h, w_qkv, s_qkv, q_out})) return RELSERVE_ERR_BAD_ARGUMENT;
-    if (workspace && (reinterpret_cast<uintptr_t>(workspace) % kAlign || workspace_bytes < (size_t)gemm_scratch_floats(T, L->qkv_dim) * 4))
-        return RELSERVE_ERR_WORKSPACE;
-    return launch_qkv_rope_append_i8(b->dev, *L, h, h_scale, w_qkv, s_qkv, q_out, cache.k_pages, cache.v_pages, static_cast<hipStream_t>(stream),
-                                     static_cast<float*>(workspace), packed != 0, kv_format(cache)) == hipSuccess
-               ? RELSERVE_OK
-               : RELSERVE_ERR_HIP;
-}
-
-int32_t relserve_layer_step_i8(const relserve_layer* L, const relserve_batch* b, const relserve_layer_weights_i8* wt, const void* x, void* y,
-                               relserve_kv_cache cache, void* workspace, size_t workspace_bytes, void* stream) {
-    drop_stale_hip_error();
-    return layer_step_int8(L, b, wt, x, y, cache, workspace, workspace_bytes, stream);
-}
-
 int32_t relserve_static_scratch_bytes(size_t* out) {
     if (!out) return RELSERVE_ERR_NULL_POINTER;
     *out = kStaticScratchBytes;
@@ -1350,53 +1108,32 @@ namespace {
 int32_t model_step(const relserve_layer* L, const relserve_batch* b, const relserve_model* m,
                    const relserve_layer_weights_w8a8* q8, const int32_t* token_ids, void* logits, void* workspace,
                    size_t workspace_bytes, void* stream) {
-    if (int32_t rc = check_pair(L, b, stream)) return rc;
-    if (!m) return RELSERVE_ERR_NULL_POINTER;
-    if (m->n_layers < 0 || m->vocab <= 0 || m->vocab % 4) return RELSERVE_ERR_BAD_ARGUMENT;
-    const int32_t T = b->dev.T, B = b->dev.num_reqs, H = L->cfg.hidden;
-    if (T == 0) return RELSERVE_OK;
-    if (!token_ids || !logits || !m->embedding || !m->w_final_norm || !m->w_lm_head) return RELSERVE_ERR_NULL_POINTER;
-    if (m->n_layers > 0 && ((!q8 && !m->layers) || !m->caches)) return RELSERVE_ERR_NULL_POINTER;
-    for (int32_t l = 0; l < m->n_layers; ++l) {
-        if (!q8) {
-            const relserve_layer_weights& w = m->layers[l];
-            if (!w.w_in_norm || !w.w_qkv || !w.w_o || !w.w_post_norm || !w.w_gate_up || !w.w_down)
-                return RELSERVE_ERR_NULL_POINTER;
+    auto check = [&](int32_t l) -> int32_t {
+        if (q8) return RELSERVE_OK;
+        const relserve_layer_weights& w = m->layers[l];
+        return w.w_in_norm && w.w_qkv && w.w_o && w.w_post_norm && w.w_gate_up && w.w_down ? RELSERVE_OK : RELSERVE_ERR_NULL_POINTER;
+    };
+    auto layers = [&](char* x, size_t layer_ws) -> int32_t {
+        bool normed = false;
+        for (int32_t l = 0; l < m->n_layers; ++l) {
+            // the next layer's input norm, if that layer can be stepped at all (what is wrong with it is for its own step to say)
+            NextNorm nn;
+            bool have_next = l + 1 < m->n_layers;
+            if (have_next && q8) {
+                nn = NextNorm{q8[l + 1].w_in_norm, L->cfg.rms_eps, nullptr, q8[l + 1].a_qkv};
+                have_next = nn.w && nn.code_scale > 0.0f && std::isfinite(nn.code_scale);
+            } else if (have_next) {
+                nn = NextNorm{m->layers[l + 1].w_in_norm, L->cfg.rms_eps};
+            }
+            NextNorm* next = have_next ? &nn : nullptr;
+            const int32_t rc = q8 ? layer_step_codes(L, b, &q8[l], x, x, m->caches[l], workspace, layer_ws, stream, normed, next)
+                                  : layer_step(L, b, &m->layers[l], x, x, m->caches[l], workspace, layer_ws, stream, normed, next);
+            if (rc) return rc;
+            normed = nn.done;
         }
-        if (int32_t rc = check_cache(b, m->caches[l])) return rc;
-    }
-    if ((int64_t)m->vocab * H >= ((int64_t)1 << 31)) return RELSERVE_ERR_TOO_LARGE;
-    if (!workspace || (reinterpret_cast<uintptr_t>(workspace) % kAlign)) return RELSERVE_ERR_WORKSPACE;
-    const size_t layer_ws = carve(*L, T, nullptr).total;
-    const size_t x_bytes = align_up((size_t)T * H * 2), last_bytes = align_up((size_t)B * H * 2);
-    if (layer_ws + x_bytes + last_bytes > workspace_bytes) return RELSERVE_ERR_WORKSPACE;
-    char* x = static_cast<char*>(workspace) + layer_ws;
-    char* h_last = x + x_bytes;
-
-    hipStream_t s = static_cast<hipStream_t>(stream);
-    if (launch_embedding(token_ids, m->embedding, m->vocab, H, T, x, s) != hipSuccess) return RELSERVE_ERR_HIP;
-    bool normed = false;
-    for (int32_t l = 0; l < m->n_layers; ++l) {   // the residual stream stays in x, rounded to bf16 between layers
-        // the next layer's input norm, if that layer can be stepped at all (what is wrong with it is for its own step to say)
-        NextNorm nn;
-        bool have_next = l + 1 < m->n_layers;
-        if (have_next && q8) {
-            nn = NextNorm{q8[l + 1].w_in_norm, L->cfg.rms_eps, nullptr, q8[l + 1].a_qkv};
-            have_next = nn.w && nn.code_scale > 0.0f && std::isfinite(nn.code_scale);
-        } else if (have_next) {
-            nn = NextNorm{m->layers[l + 1].w_in_norm, L->cfg.rms_eps};
-        }
-        NextNorm* next = have_next ? &nn : nullptr;
-        const int32_t rc = q8 ? layer_step_codes(L, b, &q8[l], x, x, m->caches[l], workspace, layer_ws, stream, normed, next)
-                              : layer_step(L, b, &m->layers[l], x, x, m->caches[l], workspace, layer_ws, stream, normed, next);
-        if (rc) return rc;
-        normed = nn.done;
-    }
-    if (launch_rmsnorm(x, false, m->w_final_norm, L->cfg.rms_eps, B, H, h_last, s, b->dev.last_tok) != hipSuccess)
-        return RELSERVE_ERR_HIP;
-    if (launch_linear(h_last, m->w_lm_head, B, m->vocab, H, 1, nullptr, logits, s) != hipSuccess)
-        return RELSERVE_ERR_HIP;
-    return RELSERVE_OK;
+        return RELSERVE_OK;
+    };
+    return model_around(L, b, m, q8 || !m ? (const void*)q8 : m->layers, token_ids, logits, workspace, workspace_bytes, stream, check, layers);
 }
 }  // namespace
 

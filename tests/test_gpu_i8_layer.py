@@ -133,6 +133,46 @@ def test_step_on_a_stream_and_captured(rs):
         assert torch.equal(y, want)
 
 
+@pytest.mark.parametrize("packed", [False, True], ids=["rowmajor", "packed"])
+def test_model_step_is_its_layers(rs, packed):
+    """Embedding, three int8 layers, final norm and output layer of the last tokens: bit for bit the calls one by one."""
+    shape, vocab, n = SHAPES["gqa"], 512, 3
+    wl = W.workload_tiny_prefix(shape=shape)
+    b = wl.batch
+    layer = rs.relserve_layer_create(shape)
+    pb = rs.relserve_batch_prepare(layer, b)
+    g = torch.Generator(device="cuda")
+    g.manual_seed(4)
+
+    def randn(*size, std=1.0, mean=0.0):
+        return (torch.randn(*size, generator=g, device="cuda") * std + mean).bfloat16()
+
+    model = {"embedding": randn(vocab, shape.hidden), "layers": [_weights(rs, shape, 50 + i, packed)[0] for i in range(n)],
+             "w_final_norm": randn(shape.hidden, std=0.02, mean=1.0), "w_lm_head": randn(vocab, shape.hidden, std=0.02)}
+    ids = torch.randint(0, vocab, (b.T,), generator=g, device="cuda", dtype=torch.int32)
+    ws = torch.empty(rs.relserve_model_workspace_bytes(layer, b.T, b.num_reqs), dtype=torch.uint8, device="cuda")
+    logits, pools = [], []
+    for whole in (True, False):
+        caches = [_pools(shape, b, 60 + i, False, rs) for i in range(n)]
+        out = torch.empty(b.num_reqs, vocab, device="cuda")
+        if whole:
+            rs.relserve_model_step(layer, pb, {**model, "caches": caches}, ids, out, ws)
+        else:
+            x = model["embedding"][ids.long()].contiguous()
+            for w, (k, v) in zip(model["layers"], caches):
+                rs.relserve_layer_step_i8(layer, pb, w, x, x, k, v, ws)
+            last = x[torch.from_numpy(np.asarray(b.q_start[1:], np.int64) - 1).cuda()].contiguous()
+            normed = torch.empty_like(last)
+            rs.relserve_rmsnorm(last, model["w_final_norm"], shape.rms_eps, normed)
+            rs.relserve_linear(normed, model["w_lm_head"], 1, None, out)
+        torch.cuda.synchronize()
+        logits.append(out)
+        pools.append([_bytes(p) for c in caches for p in c])
+    pb.close()
+    assert bool(torch.isfinite(logits[0]).all()) and torch.equal(*logits)
+    assert all(torch.equal(a, c) for a, c in zip(*pools))
+
+
 def _rotated(v, pos, base):
     """[T, heads, d] by the angles fp32(pos) * fp32(base^(-2 i / d)) in fp32, cosines in 64 bits."""
     d = v.shape[-1]
