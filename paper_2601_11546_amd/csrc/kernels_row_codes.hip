@@ -68,7 +68,7 @@ __global__ void __launch_bounds__(TPR < 256 ? 256 : TPR) row_codes_kernel(RowCod
     const int64_t base = (int64_t)row * p.n;
     // values of chunk c whose codes are taken, less the norm's factor; the stream is kept as it is normed
     float ss = 0.f, m = 0.f;
-    auto first = [&](int c, const Raw8<F32>& rx, const Raw8<false>& rd, const Raw8<false>& rw, bool store, float (&v)[8]) {
+    auto first = [&](int c, const Raw8<F32>& rx, const Raw8<false>& rd, const Raw8<false>& rw, bool mine, float (&v)[8]) {
         float s[8];
         rx.values(s);
         Raw8<F32> kept = rx;
@@ -85,7 +85,7 @@ __global__ void __launch_bounds__(TPR < 256 ? 256 : TPR) row_codes_kernel(RowCod
                 kept.values(s);
             }
         }
-        if (OP != ROWS_PLAIN && p.sum && store) {
+        if (OP != ROWS_PLAIN && p.sum && mine) {
             i32x4_t* o = reinterpret_cast<i32x4_t*>(static_cast<char*>(p.sum) + (base + 8 * (int64_t)c) * (F32 ? 4 : 2));
             if constexpr (FAR) {
                 __builtin_nontemporal_store(__builtin_bit_cast(i32x4_t, kept.lo), o);
@@ -103,13 +103,15 @@ __global__ void __launch_bounds__(TPR < 256 ? 256 : TPR) row_codes_kernel(RowCod
             rw.values(w);
 #pragma unroll
             for (int i = 0; i < 8; ++i) v[i] = s[i] * w[i];
-            if (store) {   // a chunk past the end is the last one again, which changes no maximum but would be counted twice here
+            if (mine) {   // a chunk past the end is the last one again, which would be counted twice
 #pragma unroll
                 for (int i = 0; i < 8; ++i) ss = __builtin_fmaf(s[i], s[i], ss);
             }
         }
+        if (OP != ROWS_ADD_NORM || mine) {   // (a sum in place may have reached that chunk before this read of it)
 #pragma unroll
-        for (int i = 0; i < 8; ++i) m = larger(m, v[i]);
+            for (int i = 0; i < 8; ++i) m = larger(m, v[i]);
+        }
     };
     float v[PER > 0 ? PER : 1][8];
     if constexpr (PER > 0) {

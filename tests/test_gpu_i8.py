@@ -113,6 +113,28 @@ def test_add_rmsnorm(rs, t, n, f32, delta, kept):
     _check_codes(codes, scales, values, ((n / 64 + 16) / 2 + 7) * U, 4.04 * U, f"{t} x {n}")
 
 
+@pytest.mark.parametrize("f32", [False, True])
+@pytest.mark.parametrize("n", [2056, 4104, 6152, 8200])
+def test_sum_in_place_whose_last_values_are_the_largest(rs, n, f32):
+    """Rows that end just behind a multiple of the threads, the sum written over x: threads past the end read the last chunk again, which
+    its owner may already have stored."""
+    t = 4100
+    print(f"[case] sum in place {t} x {n} f32={f32}", flush=True)
+    g = _gen(n)
+    dtype = torch.float32 if f32 else torch.bfloat16
+    x = _randn(g, t, n).to(dtype)
+    d = torch.zeros(t, n, dtype=torch.bfloat16, device="cuda")
+    d[:, -8:] = 100.0
+    w = torch.ones(n, dtype=torch.bfloat16, device="cuda")
+    want = (x.float() + d.float()).to(dtype)
+    codes, scales = torch.empty(t, n, dtype=torch.int8, device="cuda"), torch.empty(t, device="cuda")
+    rs.relserve_add_rmsnorm_i8(x, w, 1e-5, codes, scales, delta=d, sum_out=x)
+    torch.cuda.synchronize()
+    assert torch.equal(x, want)
+    s = want.double()
+    _check_codes(codes, scales, s / torch.sqrt(s.square().mean(1, keepdim=True) + 1e-5), ((n / 64 + 16) / 2 + 7) * U, 4.04 * U, f"{n}")
+
+
 @pytest.mark.parametrize("t,n", [(8300, 5136), (2500, 28680)])
 def test_rows_of_more_than_the_caches_hold(rs, t, n):
     """As above where the passes stream; 64 of the rows, and the others' codes by their range and the scale they have."""
