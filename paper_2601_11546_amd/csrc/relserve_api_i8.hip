@@ -13,28 +13,36 @@ constexpr int32_t kMaxKInt8 = 131072 - 128;
 // Codes [T, n] and, behind them, their scales [T] in a buffer of the workspace (n is a multiple of 128).
 float* scales_behind(char* codes, int64_t T, int64_t n) { return reinterpret_cast<float*>(codes + T * n); }
 
+// What is wrong with a layer's shape or weights for a step of T tokens.
+int32_t check_int8(const relserve_layer* L, const relserve_layer_weights_i8* wt, int64_t T) {
+    const relserve_layer_config& c = L->cfg;
+    for (int64_t k : {(int64_t)c.hidden, (int64_t)L->q_dim, (int64_t)c.mlp_dim})
+        if (k % 128 || k > kMaxKInt8) return RELSERVE_ERR_BAD_ARGUMENT;
+    if ((int64_t)c.mlp_dim >= 2 * (int64_t)c.hidden + 4 * (int64_t)L->q_dim) return RELSERVE_ERR_BAD_ARGUMENT;   // where the step keeps codes
+    if (T == 0) return RELSERVE_OK;
+    if (!wt->w_in_norm || !wt->w_qkv || !wt->w_o || !wt->w_post_norm || !wt->w_gate_up || !wt->w_down || !wt->s_qkv || !wt->s_o ||
+        !wt->s_gate_up || !wt->s_down)
+        return RELSERVE_ERR_NULL_POINTER;
+    if (!aligned16({wt->w_in_norm, wt->w_qkv, wt->w_o, wt->w_post_norm, wt->w_gate_up, wt->w_down, wt->s_qkv, wt->s_o, wt->s_gate_up, wt->s_down}))
+        return RELSERVE_ERR_BAD_ARGUMENT;
+    auto matrix = [&](int64_t rows, int64_t k) { return (wt->packed ? (rows + 255) / 256 * 256 : rows) * k; };
+    const int64_t largest = std::max({T * std::max({c.hidden, L->q_dim, c.mlp_dim}), matrix(L->qkv_dim, c.hidden), matrix(c.hidden, L->q_dim),
+                                      matrix(2 * (int64_t)c.mlp_dim, c.hidden), matrix(c.hidden, c.mlp_dim)});
+    return largest >= ((int64_t)1 << 31) ? RELSERVE_ERR_TOO_LARGE : RELSERVE_OK;
+}
+
 int32_t layer_step_int8(const relserve_layer* L, const relserve_batch* b, const relserve_layer_weights_i8* wt, const void* x, void* y,
                         relserve_kv_cache cache, void* workspace, size_t workspace_bytes, void* stream) {
     if (int32_t rc = check_pair(L, b, stream)) return rc;
     if (!wt) return RELSERVE_ERR_NULL_POINTER;
     if (int32_t rc = check_cache(b, cache)) return rc;
     const relserve_layer_config& c = L->cfg;
-    for (int64_t k : {(int64_t)c.hidden, (int64_t)L->q_dim, (int64_t)c.mlp_dim})
-        if (k % 128 || k > kMaxKInt8) return RELSERVE_ERR_BAD_ARGUMENT;
-    if ((int64_t)c.mlp_dim >= 2 * (int64_t)c.hidden + 4 * (int64_t)L->q_dim) return RELSERVE_ERR_BAD_ARGUMENT;   // see `act` below
     const int32_t T = b->dev.T;
+    if (int32_t rc = check_int8(L, wt, T)) return rc;
     if (T == 0) return RELSERVE_OK;
-    if (!x || !y || !wt->w_in_norm || !wt->w_qkv || !wt->w_o || !wt->w_post_norm || !wt->w_gate_up || !wt->w_down ||
-        !wt->s_qkv || !wt->s_o || !wt->s_gate_up || !wt->s_down)
-        return RELSERVE_ERR_NULL_POINTER;
-    if (!aligned16({x, y, wt->w_in_norm, wt->w_qkv, wt->w_o, wt->w_post_norm, wt->w_gate_up, wt->w_down, wt->s_qkv, wt->s_o, wt->s_gate_up, wt->s_down}))
-        return RELSERVE_ERR_BAD_ARGUMENT;
+    if (!x || !y) return RELSERVE_ERR_NULL_POINTER;
+    if (!aligned16({x, y})) return RELSERVE_ERR_BAD_ARGUMENT;
     const bool packed = wt->packed != 0;
-    const int64_t widest = std::max({c.hidden, L->q_dim, c.mlp_dim});
-    auto matrix = [&](int64_t rows, int64_t k) { return (packed ? (rows + 255) / 256 * 256 : rows) * k; };
-    if (T * widest >= ((int64_t)1 << 31) || std::max({matrix(L->qkv_dim, c.hidden), matrix(c.hidden, L->q_dim), matrix(2 * (int64_t)c.mlp_dim, c.hidden),
-                                                      matrix(c.hidden, c.mlp_dim)}) >= ((int64_t)1 << 31))
-        return RELSERVE_ERR_TOO_LARGE;
     if (!workspace || (reinterpret_cast<uintptr_t>(workspace) % kAlign)) return RELSERVE_ERR_WORKSPACE;
     Workspace w = carve(*L, T, workspace);
     if (w.total > workspace_bytes) return RELSERVE_ERR_WORKSPACE;
@@ -159,7 +167,7 @@ int32_t relserve_model_step_i8(const relserve_layer* L, const relserve_batch* b,
                                void* workspace, size_t workspace_bytes, void* stream) {
     drop_stale_hip_error();
     if (!layers) return RELSERVE_ERR_NULL_POINTER;
-    auto check = [](int32_t) -> int32_t { return RELSERVE_OK; };   // each layer's step checks its own
+    auto check = [&](int32_t l) { return check_int8(L, &layers[l], b->dev.T); };
     auto stack = [&](char* x, size_t layer_ws) -> int32_t {
         for (int32_t l = 0; l < m->n_layers; ++l)
             if (int32_t rc = layer_step_int8(L, b, &layers[l], x, x, m->caches[l], workspace, layer_ws, stream)) return rc;

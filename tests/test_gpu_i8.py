@@ -433,6 +433,19 @@ def test_feed_forward_block_captured_and_on_streams(rs):
         torch.cuda.synchronize()
 
 
+def test_no_rows(rs):
+    def empty(*size, dtype=torch.bfloat16):
+        return torch.empty(*size, dtype=dtype, device="cuda")
+
+    codes, scales = empty(0, 256, dtype=torch.int8), empty(0, dtype=torch.float32)
+    rs.relserve_quantise_rows_i8(empty(0, 256), codes, scales)
+    rs.relserve_add_rmsnorm_i8(empty(0, 256), empty(256), 1e-5, codes, scales, delta=empty(0, 256), sum_out=empty(0, 256))
+    w, ws = empty(64, 256, dtype=torch.int8), empty(64, dtype=torch.float32)
+    for epilogue, n, dtype in ((0, 64, torch.bfloat16), (1, 64, torch.float32), (2, 64, torch.bfloat16), (3, 32, torch.bfloat16)):
+        rs.relserve_linear_i8(codes, scales, w, ws, epilogue, empty(0, 64, dtype=torch.float32) if epilogue == 2 else None, empty(0, n, dtype=dtype))
+    torch.cuda.synchronize()
+
+
 def test_two_calls_at_once(rs):
     """Calls on two streams, each with a workspace of its own."""
     ps = [Product(rs, 24, 5120, 5120, True, seed=i) for i in range(2)]

@@ -173,6 +173,56 @@ def test_model_step_is_its_layers(rs, packed):
     assert all(torch.equal(a, c) for a, c in zip(*pools))
 
 
+def test_refusals_launch_nothing(rs):
+    """A layer that cannot be stepped is refused before the model step touches anything, and so are shapes and buffers that do not fit."""
+    shape = SHAPES["gqa"]
+    b = W.build_batch(shape, [3, 1], [3, 9], seed=1)
+    layer = rs.relserve_layer_create(shape)
+    pb = rs.relserve_batch_prepare(layer, b)
+    w, _ = _weights(rs, shape, 1, True)
+    x = dev_bf16(W.make_activations(b.T, shape.hidden, 1))
+    pools = _pools(shape, b, 2, False, rs)
+    ws = torch.zeros(rs.relserve_model_workspace_bytes(layer, b.T, b.num_reqs), dtype=torch.uint8, device="cuda")
+    out = torch.full((b.num_reqs, 512), 7.0, device="cuda")
+    ids = torch.zeros(b.T, dtype=torch.int32, device="cuda")
+    odd = dict(w)
+    odd["s_down"] = torch.zeros(shape.hidden + 1, device="cuda")[1:]     # not 16-byte aligned
+    model = {"embedding": x[:1].repeat(512, 1), "layers": [w, odd], "caches": [tuple(pools)] * 2, "w_final_norm": w["w_in_norm"],
+             "w_lm_head": x[:1].repeat(512, 1)}
+    before = [_bytes(p) for p in pools]
+    with pytest.raises(rs.RelserveError) as e:
+        rs.relserve_model_step(layer, pb, model, ids, out, ws)
+    assert e.value.status == -14
+    # (relserve_workspace_bytes counts 256 bytes more than a step takes)
+    for bad, status in ((ws[:rs.relserve_workspace_bytes(layer, b.T) - 512], -9), (ws[128:], -9)):
+        with pytest.raises(rs.RelserveError) as e:
+            rs.relserve_layer_step_i8(layer, pb, w, x, x, *pools, bad)
+        assert e.value.status == status
+    with pytest.raises(ValueError, match="w_o"):
+        rs.relserve_layer_step_i8(layer, pb, {**w, "w_o": w["w_o"][:-1]}, x, x, *pools, ws)
+    with pytest.raises(ValueError, match="x must"):
+        rs.relserve_layer_step_i8(layer, pb, w, x[:-1], x, *pools, ws)
+    torch.cuda.synchronize()
+    assert bool((out == 7.0).all()) and bool((ws == 0).all()) and all(torch.equal(_bytes(p), o) for p, o in zip(pools, before))
+    pb.close()
+    for bad in (W.LayerShape(256, 4, 4, 64, 688), W.LayerShape(256, 2, 2, 64, 1024)):     # mlp_dim no multiple of 128; 2 * 256 + 4 * 128
+        layer = rs.relserve_layer_create(bad)
+        b = W.build_batch(bad, [2], [2], seed=1)
+        pb = rs.relserve_batch_prepare(layer, b)
+        wt = {n: torch.zeros(s, dtype=dt, device="cuda") for n, s, dt in [
+            ("w_in_norm", (256,), torch.bfloat16), ("w_post_norm", (256,), torch.bfloat16), ("w_qkv", (bad.qkv_dim, 256), torch.int8),
+            ("s_qkv", (bad.qkv_dim,), torch.float32), ("w_o", (256, bad.q_dim), torch.int8), ("s_o", (256,), torch.float32),
+            ("w_gate_up", (2 * bad.mlp_dim, 256), torch.int8), ("s_gate_up", (2 * bad.mlp_dim,), torch.float32),
+            ("w_down", (256, bad.mlp_dim), torch.int8), ("s_down", (256,), torch.float32)]}
+        x = torch.zeros(2, 256, dtype=torch.bfloat16, device="cuda")
+        pools = [torch.zeros(b.num_pages, bad.page_size, bad.n_kv_heads, 64, dtype=torch.bfloat16, device="cuda") for _ in range(2)]
+        ws = torch.zeros(rs.relserve_workspace_bytes(layer, 2), dtype=torch.uint8, device="cuda")
+        with pytest.raises(rs.RelserveError) as e:
+            rs.relserve_layer_step_i8(layer, pb, wt, x, x, *pools, ws)
+        assert e.value.status == -14
+        pb.close()
+
+
 def _rotated(v, pos, base):
     """[T, heads, d] by the angles fp32(pos) * fp32(base^(-2 i / d)) in fp32, cosines in 64 bits."""
     d = v.shape[-1]
