@@ -244,15 +244,16 @@ int rows_tile(const GemmArgs& p, int epi) {
 
 // Weights that the last-level cache (256 MB) cannot hold beside others are read with the non-temporal hint: SwiGLU 27648 x 5120 (141 MB) 27.2 ->
 // 24.5 us.  Smaller ones may still be there from the last call: 5120 x 13824 at T = 24 13.2 with three sets in turn, 21.2 with the hint; from memory
-// (ten sets) 21.2 and 22.3, 15360 x 5120 at T = 1 15.6 and 14.6.
+// (ten sets) 21.2 and 22.3, 15360 x 5120 at T = 1 15.6 and 14.6.  Only the tile of 16 tokens has the form with
+// the hint: the others' rules end at weights of 100 MB.
 constexpr int64_t kFarWeights = (int64_t)96 << 20;
 
 template <int EPI, int D = 0>
 hipError_t run_rows(const GemmArgs& p, hipStream_t s, int tile) {
-    const bool far = p.T <= 32 && 2 * (int64_t)p.N * p.K >= kFarWeights;
+    const bool far = 2 * (int64_t)p.N * p.K >= kFarWeights;
     switch (tile) {
         case ROWS_16: return far ? launch_rows<EPI, D, 2, 1, 4, 3, true>(p, s) : launch_rows<EPI, D, 2, 1, 4, 3, false>(p, s);
-        case ROWS_32: return far ? launch_rows<EPI, D, 2, 2, 4, 2, true>(p, s) : launch_rows<EPI, D, 2, 2, 4, 2, false>(p, s);
+        case ROWS_32: return launch_rows<EPI, D, 2, 2, 4, 2, false>(p, s);
         case ROWS_64: return launch_rows<EPI, D, 2, 4, 4, 2, false>(p, s);
         case ROWS_64_SHALLOW: return launch_rows<EPI, D, 2, 4, 4, 1, false>(p, s);
         case ROWS_64_WIDE: return launch_rows<EPI, D, 4, 4, 8, 1, false>(p, s);
