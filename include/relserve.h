@@ -533,7 +533,8 @@ int32_t relserve_peak_probe_stream_pattern(const void* src, size_t bytes, int32_
 /* ---- test hook (the only one; not part of the serving interface) ----
  * Forces the tile shape and the tail split of every later GEMM launch of this process, so that tests can
  * drive each tile shape and the split-tail path on shapes the automatic choice would serve otherwise:
- * tile = 0..4 (256x256, 192x256, 128x256, 128x128, 64x128 tokens x features), -1 = automatic choice.
+ * tile = 0..5 (256x256, 192x256, 128x256, 128x128, 64x128, 160x256 tokens x features; the last one for the int8 projections, others
+ * then choose), -1 = automatic choice.
  * tail_splits = 2..8 makes the tiles of the incomplete last round split their k range that many ways
  * (0 or 1 = whole tiles only).  Shapes a tile cannot serve (the fused q/k/v epilogue needs 256 features per
  * tile) fall back to the nearest one that can.  Process-wide; the setting is one atomic word, so a launch

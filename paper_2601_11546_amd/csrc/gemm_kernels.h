@@ -939,7 +939,9 @@ __global__ void __launch_bounds__(64 * WGM * WGN) gemm_dma_kernel(GemmArgs p) {
     // that the next one adds, into registers whose last reader is over: tokens h' , weights hi, the next stage's lo and, where tokens h'
     // were, the next stage's tokens h'; so the next stage begins with h'.  Every fragment is read once, at an even rate, and the
     // stage is free (and the next one needed) at the hand-over between the second and third quarter.
-    constexpr int WH = TN / 2, AH = TM / 2, NQ = WH * AH;
+    // (An odd number of token fragments: half 0 is the larger one.)
+    constexpr int WH = TN / 2, AH = (TM + 1) / 2;
+    constexpr auto tokens = [](int half) { return half ? TM - AH : AH; };
     auto read_w = [&](Source src, int half, int i) __attribute__((always_inline)) { wf[0][half * WH + i] = read_frag(src.w, w_dist(half * WH + i)); };
     auto read_a = [&](Source src, int half, int i) __attribute__((always_inline)) { af[0][half * AH + i] = read_frag(src.a, a_dist(half * AH + i)); };
     // (Integers: the reads stand between a pair's two products of half the length.  All first halves of two pairs ahead of their second ones do
@@ -948,13 +950,15 @@ __global__ void __launch_bounds__(64 * WGM * WGN) gemm_dma_kernel(GemmArgs p) {
         const Source src = source(rd_stage, 0);
         __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-        for (int i = 0; i < 2 * NQ; ++i) {
-            const int q = i / NQ, j = i % NQ, a_half = second == (q == 0) ? 1 - h : h;
-            const int tn = (second ? WH : 0) + j / AH, tm = a_half * AH + j % AH;
+        for (int i = 0; i < WH * TM; ++i) {
+            const int n_first = WH * tokens(second ? 1 - h : h);   // products of the half step's first quarter
+            const int q = i < n_first ? 0 : 1, j = q ? i - n_first : i, a_half = second == (q == 0) ? 1 - h : h;
+            const int n_q = WH * tokens(a_half), n_a = tokens(a_half);
+            const int tn = (second ? WH : 0) + j / n_a, tm = a_half * AH + j % n_a;
             // behind every other product, or, on tiles of few products, evenly
             const bool rd_w = second == (q == 0);
-            const int nf = rd_w ? WH : AH;
-            const int f0 = 2 * nf <= NQ + 1 ? (j + 1) / 2 : j * nf / NQ, f1 = 2 * nf <= NQ + 1 ? j / 2 + 1 : (j + 1) * nf / NQ;
+            const int nf = rd_w ? WH : tokens(1 - h);
+            const int f0 = 2 * nf <= n_q + 1 ? (j + 1) / 2 : j * nf / n_q, f1 = 2 * nf <= n_q + 1 ? j / 2 + 1 : (j + 1) * nf / n_q;
             auto reads = [&]() __attribute__((always_inline)) {
 #pragma unroll
                 for (int f = f0; f < min(f1, nf); ++f) {
@@ -990,7 +994,7 @@ __global__ void __launch_bounds__(64 * WGM * WGN) gemm_dma_kernel(GemmArgs p) {
     // 64 KB.  13B layer at T = 3875 on codes: eight waves 1257 us, with the skewed ring too; four 1231, skewed 1194.)
     static_assert(!HALVES || (!F8 && NSW == NS), "halves of 16-bit tiles");
     static_assert(F8 || !FIXED || 2 * NF <= NM, "a fragment read behind every other MFMA");
-    static_assert(TN % 2 == 0 && TM % 2 == 0, "halves");
+    static_assert(TN % 2 == 0 && (QUARTERS || TM % 2 == 0), "halves");
     static_assert(!SKEW || FIXED, "the skewed ring's weights are issued in the fixed order only");
     Stage cur{0, 0};  // stage being computed
     // One k iteration (one LDS stage).  open_a, open_w: what the refill begun at the previous hand-over still issues (stage
@@ -1602,7 +1606,7 @@ hipError_t launch_small(GemmArgs p, hipStream_t s) {
 // per CU); all stages but the one being computed are in flight.
 template <int BM, int EPI, int D, int BN = 256, bool WNT = false>
 hipError_t launch_split(GemmArgs p, int splits, hipStream_t s, NextNorm* next = nullptr) {
-    constexpr int NS = BM + BN <= 192 ? 6 : BM + BN <= 256 ? 4 : BM + BN <= 320 ? 4 : BM + BN <= 384 ? 3 : 2;
+    constexpr int NS = BM + BN <= 192 ? 6 : BM + BN <= 256 ? 4 : BM + BN <= 320 ? 4 : BM + BN <= 416 ? 3 : 2;
     constexpr int NSW = weight_stages(BM, BN, NS);
     constexpr int smem = (NS * BM + NSW * BN) * 64 * 2;
     static_assert(smem <= 160 * 1024, "ring exceeds the LDS");
@@ -1739,16 +1743,20 @@ bool skinny_applies(int T, int N, int K, const float* accum) {
     return accum != nullptr && T <= SKINNY_MAX_T && K % 64 == 0 && N % 4 == 0;
 }
 
+#if RELSERVE_GEMM_INT8
+int split_rows_i8(int T, int N, int K, bool swiglu);
+#endif
 // Mid-size batches on a narrow output (W_o and W_down at a few hundred tokens): whole tiles are too few
 // for 256 CUs and splitting them through the fenced partial-tile protocol costs more than it gains, so
 // these run like the skinny path (k ranges stored to slabs, then the finish kernel) on tiles
 // of 128 rows while every tile gets at least two k ranges, or of 256 rows while it gets at least three
 // and k is long.  Returns the tile rows, 0 = not this path.  The slabs (at most 256 units x 256 x 256
-// floats) use the tail scratch.
-int split_rows(int T, int N, int K, bool has_accum) {
+// floats) use the tail scratch.  (Integers, whose sums may be cut anywhere: by the model of plan_i8.)
+int split_rows(int T, int N, int K, bool has_accum, bool swiglu) {
     if (!has_accum || T <= SKINNY_MAX_T || K % 64 || N % 4 || forced_cand() >= 0) return 0;
-    // (integers may change tiles: k up to 4096 codes is faster whole, 4096 x 4096 at T = 640 26.6 -> 25.5, at 1000 31.7 -> 27.0)
-    if (kInt8 && K <= 2048) return 0;
+#if RELSERVE_GEMM_INT8
+    return split_rows_i8(T, N, K, swiglu);
+#endif
     const int tn = (N + 255) / 256;
     if (((T + 127) / 128) * tn <= 128) return 128;
     if (((T + 255) / 256) * tn <= 85 && K >= 8192) return 256;
@@ -1762,8 +1770,12 @@ bool one_range(const GemmArgs& p, int bm) { return (kInt8 || !p.f8) && choose_sp
 
 template <int EPI>
 hipError_t launch_mid_split(GemmArgs p, int bm, hipStream_t s, NextNorm* next) {
-    if (bm == 128) return launch_split<128, EPI, 0>(p, choose_splits(p.T, p.N, p.K, 128), s, next);
-    return launch_split<256, EPI, 0>(p, choose_splits(p.T, p.N, p.K, 256), s, next);
+    const int splits = choose_splits(p.T, p.N, p.K, bm);
+    if (bm == 128) return launch_split<128, EPI, 0>(p, splits, s, next);
+    if constexpr (kInt8)
+        return bm == 160 ? launch_split<160, EPI, 0>(p, splits, s) : launch_split<192, EPI, 0>(p, splits, s);
+    else
+        return launch_split<256, EPI, 0>(p, splits, s, next);
 }
 
 // Which problems take the small kernel: those whose k the general paths never cut (the cut fixes the order of the sums), up to
@@ -1828,8 +1840,8 @@ hipError_t launch_cfg(const GemmArgs& base, hipStream_t s, const Plan& plan = Pl
         p.tiles_n = std::min(cols, p.tiles_n - col0);
     }
     constexpr int smem = 2 * (BM + BN) * BK * 2;
-    // 128 x 256 tiles are one workgroup per CU either way, so they take the third stage that fits (144 KB)
-    constexpr int DMA_BK = 64, DMA_NS = (BM == 128 && BN == 256) ? 3 : 2, DMA_NSW = weight_stages(BM, BN, DMA_NS);
+    // 128 x 256 tiles are one workgroup per CU either way, so they take the third stage that fits (144 KB; of 160 x 256 ones 156)
+    constexpr int DMA_BK = 64, DMA_NS = ((BM == 128 || BM == 160) && BN == 256) ? 3 : 2, DMA_NSW = weight_stages(BM, BN, DMA_NS);
     constexpr int dma_smem = (DMA_NS * BM + DMA_NSW * BN) * DMA_BK * 2;
     const int tiles = p.tiles_m * p.tiles_n;
     if (p.K % 64 != 0) {
@@ -1903,7 +1915,11 @@ constexpr TileCand kTiles[] = {
     // codes at hidden sizes of 5120 and more, 0.1 and 1.4 % at 256 .. 3072.  eff_swiglu: the SwiGLU projection, whose 128 x 256 tile has the
     // compiler's order and lags: 0.00 and 0.5 %.
     {256, 256, 1, 1.00f, 1.00f, 1.00f, true}, {192, 256, 1, 0.92f, 0.98f, 0.96f, true}, {128, 256, 1, 0.68f, 0.90f, 0.75f, true},
-    {128, 128, 2, 0.76f, 0.50f, 0.45f, false}, {64, 128, 3, 0.60f, 0.40f, 0.40f, false}};
+    {128, 128, 2, 0.76f, 0.50f, 0.45f, false}, {64, 128, 3, 0.60f, 0.40f, 0.40f, false},
+#if RELSERVE_GEMM_INT8
+    {160, 256, 1, 0.f, 0.f, 0.f, true},   // (integers are planned by plan_i8)
+#endif
+};
 constexpr int kTileCount = (int)(sizeof(kTiles) / sizeof(kTiles[0]));
 
 constexpr double kCuFlops = 5.2e12;          // sustained MFMA rate of one CU inside a 256 x 256 tile
@@ -1966,6 +1982,71 @@ int whole_tile(int T, int64_t n_eff, int K, bool need_bn256, bool swiglu) {
     return best;
 }
 
+#if RELSERVE_GEMM_INT8
+// Integer sums have the same bits however k is cut, so nothing holds their plans to the floats' cuts: one model of what a launch takes, in us,
+// chooses between whole tiles, tiles of the last round in k ranges, and all tiles in k ranges (split_rows).  A round of n tiles (or k ranges) on
+// 256 CUs: kSliceUs a slice of 128 codes, less the more CUs are idle (kIdle: the others then run faster), and kRoundUs; partial sums
+// written and read at kSlabMbPerUs; shapes of which a CU holds two or three take as long as the fullest CU.
+// Fitted to 3200 times of forced plans, eleven layer shapes (k of 2048 .. 28672) at 264 .. 8000 tokens: 5 % rms; with kWorth for what is less simple
+// than whole tiles, its choices among them are 0.4 % from the fastest on average.
+constexpr double kSliceUs[kTileCount] = {1.347, 1.054, 0.796, 0.449, 0.282, 0.931}, kIdle[kTileCount] = {0.30, 0.32, 0.41, 0.55, 0.66, 0.35};
+constexpr double kSwigluMore = 1.017, kRoundUs = 4.4, kLaunchUs = 3.2, kTailFinishUs = 2.0, kSlabMbPerUs = 6.9, kWorth = 0.97;
+
+double round_us_i8(int cand, int64_t n, int slices, bool swiglu) {
+    return n > 0 ? kSliceUs[cand] * (swiglu ? kSwigluMore : 1.0) * slices * (1.0 - kIdle[cand] * (1.0 - (double)n / 256.0)) + kRoundUs : 0.0;
+}
+
+double rounds_us_i8(int cand, int64_t units, int slices, bool swiglu) {
+    return (double)(units / 256) * round_us_i8(cand, 256, slices, swiglu) + round_us_i8(cand, units % 256, slices, swiglu);
+}
+
+double slabs_us_i8(int64_t values) { return (double)values * 8e-6 / kSlabMbPerUs; }   // four bytes each, written and read
+
+double whole_us_i8(int cand, int T, int64_t n_eff, int K, bool swiglu) {
+    const TileCand& c = kTiles[cand];
+    const int64_t tiles = tile_count(c, T, n_eff), slots = 256 * c.wg_per_cu;
+    if (c.wg_per_cu == 1) return kLaunchUs + rounds_us_i8(cand, tiles, K / 64, swiglu);
+    const int64_t rounds = (tiles + slots - 1) / slots;
+    const double idle = 1.0 - (double)tiles / (double)(rounds * slots);
+    return kLaunchUs + (double)rounds * (kSliceUs[cand] * (swiglu ? kSwigluMore : 1.0) * c.wg_per_cu * (K / 64) * (1.0 - kIdle[cand] * idle) + kRoundUs);
+}
+
+// *us: the plan's time, 1 / kWorth of it where tiles are cut
+Plan plan_i8(int T, int64_t n_eff, int K, bool need_bn256, bool allow_tail, bool swiglu, double* us) {
+    Plan best{0, 0, 1};
+    *us = 1e300;
+    for (int i = 0; i < kTileCount; ++i) {
+        const TileCand& c = kTiles[i];
+        if (need_bn256 && !c.qkv) continue;
+        const double whole = whole_us_i8(i, T, n_eff, K, swiglu);
+        if (whole < *us) *us = whole, best = Plan{i, 0, 1};
+        if (!allow_tail || c.wg_per_cu > 1) continue;
+        const int64_t tiles = tile_count(c, T, n_eff), rem = tiles % 256;
+        const int slices = K / 64;
+        for (int sp = 2; rem > 0 && sp <= 8 && slices / sp >= 8 && rem * sp * c.bm * c.bn <= kTailFloats; ++sp) {
+            const double t = kLaunchUs + rounds_us_i8(i, tiles - rem, slices, swiglu) + rounds_us_i8(i, rem * sp, (slices + sp - 1) / sp, swiglu) +
+                             slabs_us_i8(rem * sp * c.bm * c.bn) + kTailFinishUs;
+            if (t / kWorth < *us) *us = t / kWorth, best = Plan{i, (int)rem, sp};
+        }
+    }
+    return best;
+}
+
+int split_rows_i8(int T, int N, int K, bool swiglu) {
+    double best_us;
+    plan_i8(T, N, K, false, true, swiglu, &best_us);
+    int rows = 0;
+    for (int i : {1, 2, 5}) {   // (256 rows were never ahead by more than 2 %)
+        const int bm = kTiles[i].bm, splits = choose_splits(T, N, K, bm);
+        if (splits < 2) continue;
+        const double t = (kLaunchUs + rounds_us_i8(i, tile_count(kTiles[i], T, N) * splits, (K / 64 + splits - 1) / splits, swiglu) +
+                          slabs_us_i8((int64_t)T * N * splits)) / kWorth;
+        if (t < best_us) best_us = t, rows = bm;
+    }
+    return rows;
+}
+#endif
+
 // Whole tiles of two shapes: the last round of a launch is half empty on average, and what it leaves idle can be had by giving its
 // columns of tiles to a launch of smaller tiles that fill one round more evenly (any shape gives the same bits).  For each number of
 // full rounds of each 256-feature shape: as many columns as they hold, the rest on another; taken where the model that
@@ -1975,24 +2056,29 @@ int whole_tile(int T, int64_t n_eff, int K, bool need_bn256, bool swiglu) {
 // profiles/gemm_whole_tiles.txt), of 70 more at k (in 2-byte units) of 768 .. 2304 4.7 % and one loss of 2.6.  (Below a modelled gain of
 // 4 % the second launch lost 1 - 3 % as often as it won them.)
 constexpr double kSecondLaunchSec = 6e-6, kTwoShapesGain = 0.04;
-void two_shapes(int T, int64_t n_eff, int K, bool swiglu, Plan* plan) {
+// (Integers: against the time of whatever plan there is, cut or whole, with the model of plan_i8, which counts both launches.)
+void two_shapes(int T, int64_t n_eff, int K, bool swiglu, Plan* plan, double plan_us = 0.0) {
     const int cols = (int)((n_eff + 255) / 256);
     auto cost = [&](int cand, int c) {
+#if RELSERVE_GEMM_INT8
+        return 1e-6 * whole_us_i8(cand, T, (int64_t)c * 256, K, swiglu);
+#endif
         const TileCand& t = kTiles[cand];
         const int64_t tiles = (int64_t)((T + t.bm - 1) / t.bm) * c, rounds = (tiles + 255) / 256;
         return (double)rounds * (tile_sec(t, K, swiglu ? t.eff_swiglu : t.eff) + kRoundSec) / (t.bm >= 256 ? idle_boost(tiles, 256) : 1.0);
     };
-    if (plan->cand > 2) return;
-    double best = cost(plan->cand, cols) * (1.0 - kTwoShapesGain) - kSecondLaunchSec;
-    for (int a = 0; a < 3; ++a) {
+    if (!kInt8 && !kTiles[plan->cand].qkv) return;
+    double best = kInt8 ? 1e-6 * plan_us * 0.97 : cost(plan->cand, cols) * (1.0 - kTwoShapesGain) - kSecondLaunchSec;
+    for (int a = 0; a < kTileCount; ++a) {
+        if (!kTiles[a].qkv) continue;
         const int rows = (T + kTiles[a].bm - 1) / kTiles[a].bm;
         for (int rounds = 1; rounds * 256 / rows < cols; ++rounds) {
             const int c = rounds * 256 / rows;
             if (c == 0) continue;
-            for (int b = 0; b < 3; ++b) {
-                if (b == a) continue;
+            for (int b = 0; b < kTileCount; ++b) {
+                if (b == a || !kTiles[b].qkv) continue;
                 const double t = cost(a, c) + cost(b, cols - c);
-                if (t < best) best = t, plan->cols1 = c, plan->cand1 = a, plan->cand2 = b;
+                if (t < best) best = t, plan->cols1 = c, plan->cand1 = a, plan->cand2 = b, plan->tail_tiles = 0;
             }
         }
     }
@@ -2017,6 +2103,12 @@ bool forced_plan(int T, int64_t n_eff, int K, bool need_bn256, bool allow_tail, 
 Plan plan_for(int T, int64_t n_eff, int K, bool need_bn256, bool allow_tail, bool swiglu) {
     Plan plan;
     if (forced_plan(T, n_eff, K, need_bn256, allow_tail, &plan)) return plan;
+#if RELSERVE_GEMM_INT8
+    double us;
+    plan = plan_i8(T, n_eff, K, need_bn256, allow_tail, swiglu, &us);
+    two_shapes(T, n_eff, K, swiglu, &plan, us);
+    return plan;
+#endif
     plan = choose_cut(T, n_eff, K, need_bn256, allow_tail);
     if (plan.tail_tiles == 0 && !(swiglu && K < swiglu_fit_k(T))) plan.cand = whole_tile(T, n_eff, K, need_bn256, swiglu);
     if (plan.tail_tiles == 0 && K % 64 == 0) two_shapes(T, n_eff, K, swiglu, &plan);   // (the kernel for other k knows no columns)
@@ -2036,6 +2128,9 @@ hipError_t launch_epi(const GemmArgs& p, hipStream_t s) {
     const int64_t n_eff = EPI == EPI_SWIGLU ? 2 * (int64_t)p.n_half : p.N;
     const Plan plan = plan_for(p.T, n_eff, p.K, false, p.accum != nullptr, EPI == EPI_SWIGLU);
     return run_plan(plan, [&](int cand, int col0, int cols) {
+        if constexpr (kInt8) {
+            if (cand == 5) return launch_cfg<160, 256, EPI>(p, s, plan, col0, cols);
+        }
         switch (cand) {
             case 0: return launch_cfg<256, 256, EPI>(p, s, plan, col0, cols);
             case 1: return launch_cfg<192, 256, EPI>(p, s, plan, col0, cols);
@@ -2068,7 +2163,7 @@ hipError_t run_linear(const GemmArgs& p, int epilogue, hipStream_t s, NextNorm* 
             default: return hipErrorInvalidValue;
         }
     }
-    const int bm = split_rows(p.T, p.N, p.K, p.accum != nullptr);
+    const int bm = split_rows(p.T, p.N, p.K, p.accum != nullptr, epilogue == EPI_SWIGLU);
     if (bm && !one_range(p, bm)) {
         switch (epilogue) {
             case EPI_BF16: return launch_mid_split<EPI_BF16>(p, bm, s, next);
@@ -2093,6 +2188,9 @@ hipError_t launch_qkv_d(const GemmArgs& p, hipStream_t s) {
     if (p.T <= 64) return launch_cfg<64, 256, EPI_QKV_ROPE, D>(p, s);
     const Plan plan = plan_for(p.T, p.N, p.K, true, p.accum != nullptr, false);   // the rotation needs 128 features per wave
     return run_plan(plan, [&](int cand, int col0, int cols) {
+        if constexpr (kInt8) {
+            if (cand == 5) return launch_cfg<160, 256, EPI_QKV_ROPE, D>(p, s, plan, col0, cols);
+        }
         switch (cand) {
             case 0: return launch_cfg<256, 256, EPI_QKV_ROPE, D>(p, s, plan, col0, cols);
             case 1: return launch_cfg<192, 256, EPI_QKV_ROPE, D>(p, s, plan, col0, cols);

@@ -5,7 +5,7 @@
 namespace relserve {
 
 void gemm_force_plan(int cand, int splits) {
-    g_forced_plan.store(cand < 0 ? -1 : (cand | (splits << 8)), std::memory_order_relaxed);
+    g_forced_plan.store(cand < 0 || cand >= kTileCount ? -1 : (cand | (splits << 8)), std::memory_order_relaxed);
     gemm_force_plan_i8(cand, splits);
 }
 

@@ -302,6 +302,26 @@ def test_every_tile_and_split_gives_the_same_bits(rs, tile, splits):
         rs.relserve_debug_force_gemm_plan()
 
 
+@pytest.mark.parametrize("splits", [0, 2, 4])
+@pytest.mark.parametrize("t,n,k", [(1, 512, 128), (159, 1284, 256), (160, 1008, 384), (161, 512, 512), (320, 1284, 640), (333, 1008, 4096), (700, 1284, 4096)])
+def test_the_tile_of_160_tokens_gives_the_same_bits(rs, t, n, k, splits):
+    """An odd number of token fragments a wave, of all lengths of its ring of three stages."""
+    for packed in (False, True):
+        p = Product(rs, t, n, k, packed)
+        for e in (0, 1, 2, 3):
+            if e == 3 and n % 16:
+                continue
+            print(f"[case] linear i8 T={t} N={n} K={k} epilogue {e} packed={packed} splits {splits}", flush=True)
+            want = p.check(e, p.workspace())
+            try:
+                rs.relserve_debug_force_gemm_plan(5, splits)
+                got = p.check(e, p.workspace())
+            finally:
+                rs.relserve_debug_force_gemm_plan()
+            if e in (0, 3):     # (the others' residuals are drawn anew)
+                assert torch.equal(got, want)
+
+
 @pytest.mark.parametrize("t,n,k,e", [(1, 5120, 5120, 0), (16, 1004, 1280, 0), (24, 2056, 2048, 0), (32, 27648, 4096, 3), (33, 512, 384, 0), (64, 10240, 2048, 0),
                                      (60, 5124, 4096, 0), (100, 6000, 128, 0), (200, 2816, 1152, 3), (900, 520, 640, 0), (2, 57344, 2048, 3), (130, 10000, 2176, 0), (128, 11264, 5120, 3),
                                      (75, 7172, 4096, 0), (250, 3600, 5120, 3), (640, 2560, 4096, 0)])

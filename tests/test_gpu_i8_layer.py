@@ -284,6 +284,31 @@ def test_qkv_rope_append(rs, name, n_dec, chunk, packed):
     pb.close()
 
 
+@pytest.mark.parametrize("name,n_dec,chunk", [("mha", 3, 100), ("g4d128", 10, 150), ("gqa", 7, 600)])
+def test_qkv_rope_append_on_the_tile_of_160_tokens(rs, name, n_dec, chunk):
+    shape = SHAPES[name]
+    b = W.build_batch(shape, [1] * n_dec + [chunk], [5 + i for i in range(n_dec)] + [chunk + 3], seed=n_dec + chunk)
+    layer = rs.relserve_layer_create(shape)
+    pb = rs.relserve_batch_prepare(layer, b)
+    w, _ = _weights(rs, shape, 1, True)
+    x = dev_bf16(W.make_activations(b.T, shape.hidden, 1))
+    h, hs = torch.empty(b.T, shape.hidden, dtype=torch.int8, device="cuda"), torch.empty(b.T, device="cuda")
+    rs.relserve_quantise_rows_i8(x, h, hs)
+    got = []
+    for tile in (0, 5):
+        pools, q = _pools(shape, b, 9, False, rs), torch.zeros(b.T, shape.q_dim, dtype=torch.bfloat16, device="cuda")
+        print(f"[case] q/k/v i8 {name} T={b.T} tile {tile}", flush=True)
+        try:
+            rs.relserve_debug_force_gemm_plan(tile, 0)
+            rs.relserve_qkv_rope_append_i8(layer, pb, h, hs, w["w_qkv"], w["s_qkv"], q, *pools, packed=True)
+        finally:
+            rs.relserve_debug_force_gemm_plan()
+        torch.cuda.synchronize()
+        got.append([q] + [_bytes(p) for p in pools])
+    assert all(torch.equal(a, c) for a, c in zip(*got))
+    pb.close()
+
+
 def _rows64(v):
     m = v.abs().amax(1, keepdim=True) / 127.0
     return torch.round(v / m) * m
