@@ -302,6 +302,29 @@ def test_every_tile_and_split_gives_the_same_bits(rs, tile, splits):
         rs.relserve_debug_force_gemm_plan()
 
 
+@pytest.mark.parametrize("t,n,k,e", [(640, 1280, 5120, 1), (265, 2564, 13824, 2), (320, 8192, 13824, 0), (900, 2564, 8192, 0), (1900, 20480, 2048, 3),
+                                     (780, 10240, 1024, 0), (500, 20480, 1024, 3), (780, 15360, 2048, 0)])
+def test_plans_of_more_tokens(rs, t, n, k, e):
+    """Tails and whole problems in k ranges, two tile shapes side by side, whole tiles of each shape: a forced tile's bits, with scratch and without."""
+    print(f"[case] linear i8 T={t} N={n} K={k} epilogue {e}", flush=True)
+    p = Product(rs, t, n, k, True)
+    dtype = torch.float32 if e == 1 else torch.bfloat16
+    res = _randn(p.g, t, n).to(torch.bfloat16 if e == 1 else torch.float32) if e in (1, 2) else None
+    got = []
+    p.check(e, p.workspace())
+    for force, workspace in ((False, p.workspace()), (False, None), (True, None)):
+        out = torch.empty(t, n // 2 if e == 3 else n, dtype=dtype, device="cuda")
+        try:
+            if force:
+                rs.relserve_debug_force_gemm_plan(2, 0)
+            p.call(e, res, out, workspace)
+        finally:
+            rs.relserve_debug_force_gemm_plan()
+        got.append(out)
+    torch.cuda.synchronize()
+    assert torch.equal(got[0], got[2]) and torch.equal(got[1], got[2])
+
+
 @pytest.mark.parametrize("splits", [0, 2, 4])
 @pytest.mark.parametrize("t,n,k", [(1, 512, 128), (159, 1284, 256), (160, 1008, 384), (161, 512, 512), (320, 1284, 640), (333, 1008, 4096), (700, 1284, 4096)])
 def test_the_tile_of_160_tokens_gives_the_same_bits(rs, t, n, k, splits):
