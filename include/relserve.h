@@ -321,8 +321,10 @@ int32_t relserve_linear_w8a8(const void* a, const void* w, const float* w_scale,
  * relserve_layer_weights_w8a8 is, without calibration: a token's scale is taken from the token itself) ----
  * Row t of codes [T, n] (int8) with scales [T] (fp32) stands for codes[t, i] * scales[t].  A row is made with
  *     scale = m / 127, m = the row's largest magnitude;  code = the integer nearest to value * 127 / m (ties to even)
- * so codes lie in [-127, 127].  A row of zeros has scale 0 and codes of 0; one with a NaN or an infinity has a scale that is not finite
- * and codes of 0: whatever is computed from it is not finite either.
+ * so codes lie in [-127, 127].  Codes of bf16 rows are exactly these, and so are those of norms of bf16 streams, with s * w (below) as the
+ * value, since the norm's factor cancels; a norm of an fp32 stream rounds s * w and the quotient to fp32 first.
+ * A row of zeros has scale 0 and codes of 0; one with a NaN or an infinity has a scale that is not finite and codes of 0: whatever is computed
+ * from it is not finite either.
  * All pointers are device memory, 16-byte aligned but for the scales of tokens (RELSERVE_ERR_BAD_ARGUMENT otherwise).
  *
  * relserve_quantise_rows_i8: codes and scales of the rows of in [n_rows, n] bf16 (activations, or weights: rows are output channels).

@@ -163,10 +163,16 @@ __global__ void __launch_bounds__(TPR < 256 ? 256 : TPR) row_codes_kernel(RowCod
     }
     const float inv = OP != ROWS_PLAIN ? 1.0f / sqrtf(ss / (float)p.n + p.eps) : 1.0f;
     if (lane == 0) p.scales[row] = m * inv / 127.0f;
-    // 127 / m overflows for the smallest magnitudes: these are lifted by 2^100 first.  Nothing to scale by (0, infinite, NaN): codes of 0.
-    const bool some = m > 0.0f && m < INFINITY, tiny = m < 0x1p-100f;
-    const float per = some ? 127.0f / (tiny ? m * 0x1p100f : m) : 0.0f;
-    // v * per + 1.5 * 2^23 in one rounding is the nearest integer, ties to even, and its low byte the code
+    // Nothing to scale by (0, infinite, NaN): codes of 0.  127 / m overflows for the smallest magnitudes, and what it lacks is no normal
+    // number for the largest: such rows are moved by a power of two first.
+    const bool some = m > 0.0f && m < INFINITY;
+    const float move = m < 0x1p-100f ? 0x1p100f : m > 0x1p60f ? 0x1p-100f : 1.0f, top = m * move;
+    // The quotient from 127 / m and from what that lacks: its product alone would put quotients of an integer and a half (in bf16 rows every
+    // |v| = m / 2 is 63.5) on either side.  It is rounded to 24 bits once, from within 2^-45 of its value, and no other quotient of two bf16
+    // values, or of two products of such, is near enough to an integer and a half to become one by that.  (Two instructions a value more than
+    // the product alone, us: rows 4099 x 28672 56.4 -> 56.9, 60 x 53248 5.7 -> 6.3; add + norm 8192 x 8192 71.0 -> 71.1, norm 4096 x 1024 3.8 -> 3.9.)
+    const float per = some ? 127.0f / top : 0.0f, lack = __builtin_fmaf(-per, top, 127.0f) * (per * (1.0f / 127.0f));
+    // quotient + 1.5 * 2^23 is the nearest integer, ties to even, and its low byte the code
     auto codes = [&](int c, float (&u)[8]) {
         uint32_t o[2];
 #pragma unroll
@@ -174,8 +180,9 @@ __global__ void __launch_bounds__(TPR < 256 ? 256 : TPR) row_codes_kernel(RowCod
             uint32_t b[4];
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                if (tiny) u[4 * h + i] *= 0x1p100f;
-                b[i] = __float_as_uint(__builtin_fmaf(u[4 * h + i], per, 12582912.0f));
+                float v = u[4 * h + i];
+                if (move != 1.0f) v *= move;
+                b[i] = __float_as_uint(__builtin_fmaf(v, per, v * lack) + 12582912.0f);
             }
             const uint32_t lo = __builtin_amdgcn_perm(b[1], b[0], 0x0c0c0400u), hi = __builtin_amdgcn_perm(b[3], b[2], 0x04000c0cu);
             o[h] = some ? lo | hi : 0u;
