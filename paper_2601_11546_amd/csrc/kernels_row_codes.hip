@@ -5,6 +5,7 @@
 // The norm's factor 1 / rms is the same for the whole row, so it cancels in value * 127 / m: the codes come from s * w alone, and the sum of
 // squares, which is done with the largest magnitude in one reduction, goes into the scale only.
 // Memory bound: every byte once.  A row's values stay in registers between the reduction and the codes.
+#include <algorithm>
 #include <type_traits>
 
 #include "device_utils.h"
@@ -243,10 +244,23 @@ template <bool F32, int OP>
 hipError_t launch_rows(const RowCodesArgs& p, hipStream_t s) {
     const int chunks = p.n / 8;
     const int64_t bytes = (int64_t)p.rows * p.n * ((F32 ? 4 : 2) * (OP == ROWS_ADD_NORM && p.sum ? 2 : 1) + (OP == ROWS_ADD_NORM ? 2 : 0) + 1);
+    // A launch counts its threads in 32 bits, and one of more (2^26 + 5 rows of 8 values) leaves rows out without an error: at most 2^31 in one.
     auto go = [&](auto kernel, int tpr) {
-        const int per_block = tpr < 256 ? 256 / tpr : 1;
-        kernel<<<dim3((p.rows + per_block - 1) / per_block), dim3(tpr < 256 ? 256 : tpr), 0, s>>>(p);
-        return hipGetLastError();
+        const int per_block = tpr < 256 ? 256 / tpr : 1, most = (int)(((int64_t)1 << 31) / tpr);
+        auto behind = [&](const void* base, int64_t bytes) { return base ? (void*)(static_cast<const char*>(base) + bytes) : nullptr; };
+        for (int at = 0; at < p.rows; at += most) {
+            RowCodesArgs q = p;
+            const int64_t skip = (int64_t)at * p.n;
+            q.rows = std::min(most, p.rows - at);
+            q.x = behind(p.x, skip * (F32 ? 4 : 2));
+            q.delta = static_cast<const uint16_t*>(behind(p.delta, skip * 2));
+            q.sum = behind(p.sum, skip * (F32 ? 4 : 2));
+            q.codes += skip;
+            q.scales += at;
+            kernel<<<dim3((q.rows + per_block - 1) / per_block), dim3(tpr < 256 ? 256 : tpr), 0, s>>>(q);
+            if (hipError_t e = hipGetLastError()) return e;
+        }
+        return hipSuccess;
     };
     if (chunks <= 64) return go(row_codes_kernel<F32, OP, 64, 1>, 64);
     if (p.rows >= 1024) {   // one workgroup of four rows per CU

@@ -79,3 +79,47 @@ def test_ties_are_as_frequent_as_ordinary_rows_have_them(rs, t, n):
     rs.relserve_quantise_rows_i8(x, codes, scales)
     torch.cuda.synchronize()
     assert torch.equal(codes, _want(x.double()))
+
+
+ROWS = 2 ** 26 + 5      # of 64 threads each: 2^32 threads and a few more, which one launch cannot count
+
+
+def _many(dtype, period, fill):
+    """ROWS rows of 8 values that repeat after an odd number of them."""
+    return fill(period).to(dtype).repeat(-(-ROWS // period), 1)[:ROWS].contiguous()
+
+
+def _all_periods_alike(out, period):
+    whole = ROWS // period * period
+    return bool((out[:whole].view(-1, period, *out.shape[1:]) == out[:period]).all()) and torch.equal(out[whole:], out[:ROWS - whole])
+
+
+def test_more_rows_than_a_launch_has_threads_for(rs):
+    """Every row of a GB of short ones is written, by its own values: rows, and the norm with its sum in place."""
+    g = torch.Generator(device="cuda")
+    g.manual_seed(1)
+    period = 2 ** 20 + 1
+    x = _many(torch.bfloat16, period, lambda n: torch.randn(n, 8, generator=g, device="cuda"))
+    codes, scales = torch.full((ROWS, 8), 77, dtype=torch.int8, device="cuda"), torch.full((ROWS,), -3.0, device="cuda")
+    print(f"[case] rows {ROWS} x 8", flush=True)
+    rs.relserve_quantise_rows_i8(x, codes, scales)
+    torch.cuda.synchronize()
+    assert torch.equal(codes[:period], _want(x[:period].double()))
+    # m / 127 rounded once (in 32 bits torch divides by a number as it multiplies with its rounded reciprocal; the quotient of 53 bits is not
+    # within a rounding of halfway between two of 24, from which m / 127 is 2^-32 of its value at least)
+    assert torch.equal(scales[:period], (x[:period].double().abs().amax(1) / 127.0).float())
+    assert _all_periods_alike(codes, period) and _all_periods_alike(scales, period)
+    d = _many(torch.bfloat16, period, lambda n: torch.randn(n, 8, generator=g, device="cuda"))
+    w = torch.tensor([1.0, 0.5, 1.5, 1.0, 2.0, 0.75, 1.25, 1.0], device="cuda").to(torch.bfloat16)
+    want = (x[:period].float() + d[:period].float()).to(torch.bfloat16)
+    codes.fill_(77)
+    scales.fill_(-3.0)
+    print(f"[case] norm {ROWS} x 8, the sum in place", flush=True)
+    rs.relserve_add_rmsnorm_i8(x, w, 1e-5, codes, scales, delta=d, sum_out=x)
+    torch.cuda.synchronize()
+    s = want.double()
+    m = (s * w.double()).abs().amax(1) / torch.sqrt(s.square().mean(1) + 1e-5)
+    assert torch.equal(x[:period], want) and torch.equal(codes[:period], _want(s * w.double()))
+    # squares of eight values in one chain, 63 additions of the lanes' zeros, root, reciprocal, m, its product, the division
+    assert bool(((scales[:period].double() - m / 127.0).abs() <= 12 * U * m / 127.0).all())
+    assert _all_periods_alike(x, period) and _all_periods_alike(codes, period) and _all_periods_alike(scales, period)
