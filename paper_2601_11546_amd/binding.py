@@ -423,6 +423,21 @@ def _dense(where: str, *tensors) -> None:
         raise ValueError(f"{where}: the tensors do not lie on the current device")
 
 
+def _pools(layer, k_pages, v_pages):
+    """What _dense expects of a cache's pools: as many pages each, 16-bit, or 8-bit codes in a QuantPool."""
+    s = layer.shape
+    for name, pool in (("k_pages", k_pages), ("v_pages", v_pages)):
+        t, dtype = pool, torch.bfloat16
+        if isinstance(pool, QuantPool):
+            t, dtype = pool.codes, torch.float8_e4m3fn if pool.codes.dtype is torch.float8_e4m3fn else torch.uint8
+        yield name, t, dtype, (k_pages.shape[0], s.page_size, s.n_kv_heads, s.head_dim)
+
+
+def _scratch(workspace):
+    """And of a workspace, whose size in bytes is all that counts."""
+    return "workspace", workspace, workspace.dtype, workspace.shape
+
+
 def _address(t):
     return None if t is None else t.data_ptr()
 
@@ -481,7 +496,7 @@ def relserve_qkv_rope_append_i8(layer, pbatch, h, h_scale, w_qkv, s_qkv, q_out, 
     _dense("relserve_qkv_rope_append_i8", ("h", h, torch.int8, (pbatch.T, layer.shape.hidden)), ("h_scale", h_scale, torch.float32, (t,)),
            ("w_qkv", w_qkv, torch.int8, ((rows + 255) // 256 * 256 * k,) if packed else (rows, k)),
            ("s_qkv", s_qkv, torch.float32, (layer.shape.qkv_dim,)), ("q_out", q_out, torch.bfloat16, (t, layer.shape.q_dim)),
-           ("workspace", workspace, torch.uint8, workspace.shape if workspace is not None else ()))
+           ("workspace", workspace, torch.uint8, workspace.shape if workspace is not None else ()), *_pools(layer, k_pages, v_pages))
     _check(_lib.relserve_qkv_rope_append_i8(layer.handle, pbatch.handle, h.data_ptr(), h_scale.data_ptr(), w_qkv.data_ptr(), s_qkv.data_ptr(),
                                             q_out.data_ptr(), _cache(k_pages, v_pages), bool(packed), _address(workspace),
                                             0 if workspace is None else workspace.numel(), _stream_address(h, stream)),
@@ -513,7 +528,8 @@ def _weights_i8(layer, w: dict) -> LayerWeightsI8:
 def relserve_layer_step_i8(layer, pbatch, weights: dict, x, y, k_pages, v_pages, workspace, stream=None) -> None:
     """weights: as quantise_layer_weights_i8 makes them, or these packed by pack_layer_weights_w8a8."""
     shape = (pbatch.T, layer.shape.hidden)
-    _dense("relserve_layer_step_i8", ("x", x, torch.bfloat16, shape), ("y", y, torch.bfloat16, shape))
+    _dense("relserve_layer_step_i8", ("x", x, torch.bfloat16, shape), ("y", y, torch.bfloat16, shape), *_pools(layer, k_pages, v_pages),
+           _scratch(workspace))
     wt = _weights_i8(layer, weights)
     _check(_lib.relserve_layer_step_i8(layer.handle, pbatch.handle, C.byref(wt), x.data_ptr(), y.data_ptr(), _cache(k_pages, v_pages),
                                        workspace.data_ptr(), workspace.numel() * workspace.element_size(), _stream_address(x, stream)),
@@ -542,6 +558,7 @@ def relserve_model_step(layer, pbatch, model: dict, token_ids, logits, workspace
     int8 = w8a8 and "a_qkv" not in model["layers"][0]
     lc = (KVCache * n)(*[_cache(k, v) for k, v in model["caches"]])
     if int8:
+        _dense("relserve_model_step_i8", _scratch(workspace), *(p for k, v in model["caches"] for p in _pools(layer, k, v)))
         lw = (LayerWeightsI8 * n)(*[_weights_i8(layer, w) for w in model["layers"]])
         m = Model(n, model["embedding"].shape[0], model["embedding"].data_ptr(), None,
                   C.cast(lc, C.c_void_p), model["w_final_norm"].data_ptr(), model["w_lm_head"].data_ptr())
