@@ -336,7 +336,7 @@ int32_t relserve_linear_w8a8(const void* a, const void* w, const float* w_scale,
  *
  * relserve_linear_i8: out[t, n] = (sum_k a[t, k] * w[n, k]) * (w_scale[n] * a_scale[t]): a [T, K], w [N, K] int8 (any codes, -128 too),
  * the sum exact in 32 bits (and so the same bits whatever tiles and splits compute it), then fp32; epilogues, residuals and outputs as
- * relserve_linear.  K a multiple of 128, at most 130944 (RELSERVE_ERR_TOO_LARGE above), N of 4 (of 16 for SwiGLU).  packed != 0: w is
+ * relserve_linear (epilogues 0 and 3 read no residual).  K a multiple of 128, at most 130944 (RELSERVE_ERR_TOO_LARGE above), N of 4 (of 16 for SwiGLU).  packed != 0: w is
  * relserve_pack_weight applied to the matrix seen as [N, K / 2] two-byte units.  workspace: scratch as in relserve_layer_step, of at least
  * relserve_linear_i8_workspace_bytes(T, N) bytes: lets the k range of a few tokens' product be computed by several workgroups; or NULL (few
  * tokens are then slower). */

@@ -75,3 +75,11 @@ def test_workspaces(rs, call):
         call(rs, ws=torch.zeros(128, dtype=torch.uint8)[::2])
     with pytest.raises(ValueError, match="current device"):
         call(rs, ws=torch.zeros(16, dtype=torch.float32))
+
+
+def test_a_residual_that_the_epilogue_does_not_add(rs):
+    a, scale, w, w_scale = torch.zeros(4, 128, dtype=torch.int8), torch.zeros(4), torch.zeros(64, 128, dtype=torch.int8), torch.zeros(64)
+    for epilogue, n in ((0, 64), (3, 32)):
+        for dtype in (torch.float32, torch.bfloat16):
+            with pytest.raises(ValueError, match="residual"):
+                rs.relserve_linear_i8(a, scale, w, w_scale, epilogue, torch.zeros(4, 64, dtype=dtype), torch.zeros(4, n, dtype=torch.bfloat16))
