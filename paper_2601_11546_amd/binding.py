@@ -390,10 +390,11 @@ def relserve_linear_w8a8(a, w, w_scale, a_scale: float, epilogue: int, residual,
 
 
 def pack_codes(w):
-    """An [N, K] code matrix (uint8, or the int8 projections' integers) in the packed layout: relserve_pack_weight on its rows seen as K / 2 two-byte units."""
+    """An [N, K] code matrix in the packed layout: relserve_pack_weight on its rows seen as K / 2 two-byte units.  The int8 projections' integers
+    stay int8, other codes come as uint8."""
     import torch
     n, k = w.shape
-    packed = torch.empty(relserve_packed_weight_elems(n, k // 2) * 2, dtype=w.dtype, device=w.device)
+    packed = torch.empty(relserve_packed_weight_elems(n, k // 2) * 2, dtype=torch.int8 if w.dtype is torch.int8 else torch.uint8, device=w.device)
     _check(_lib.relserve_pack_weight(_ptr(w), n, k // 2, _ptr(packed), _stream(None)), "relserve_pack_weight")
     return packed
 
