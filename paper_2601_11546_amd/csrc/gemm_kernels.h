@@ -1685,19 +1685,15 @@ hipError_t launch_skinny_whole(GemmArgs p, hipStream_t s) {
     return of_operands(p, go);
 }
 
-template <int EPI, int D>
-hipError_t launch_skinny(const GemmArgs& p, hipStream_t s, NextNorm* next = nullptr) {
-    if (p.T <= 128) {
+// k ranges of such a projection, the ways the sums are cut; 0: whole tiles that fill the CUs.
+int skinny_ranges(int T, int N, int K, bool swiglu) {
+    if (T <= 128) {
         // One token tile: the MFMA work is small next to the weight stream, so 128-feature tiles cost nothing
         // and need half the k splits (half the slab traffic); the gate/up projection has enough of them to
         // fill the CUs unsplit and runs the fused kernel.
-        if constexpr (EPI == EPI_SWIGLU) {
-            const int tiles = (p.n_half + 63) / 64, rounds = (tiles + 255) / 256;
-            if (tiles >= 0.8 * 256 * rounds)
-                return p.T <= 64 ? launch_skinny_whole<64, EPI>(p, s) : launch_skinny_whole<128, EPI>(p, s);
-        }
-        if (p.T <= 64) return launch_split<64, EPI, D, 128, true>(p, choose_splits(p.T, p.N, p.K, 64, 128), s, next);
-        return launch_split<128, EPI, D, 128, true>(p, choose_splits(p.T, p.N, p.K, 128, 128), s, next);
+        const int tiles = (N / 2 + 63) / 64, rounds = (tiles + 255) / 256;
+        if (swiglu && tiles >= 0.8 * 256 * rounds) return 0;
+        return choose_splits(T, N, K, T <= 64 ? 64 : 128, 128);
     }
     // 129 .. 256 tokens: one token tile of 192 or 256 rows x 128 features, so that every weight is read once (two tiles of
     // 128 rows read them twice; what the CUs draw from the L2 is the bound here, weights and activations together).
@@ -1705,8 +1701,21 @@ hipError_t launch_skinny(const GemmArgs& p, hipStream_t s, NextNorm* next = null
     // 248 -> 208 us at T = 160, 253 -> 232 at 200, 265 -> 239 at 256 (with an event pair per launch).
     // The k ranges are those of 128 x 256 tiles (never fewer tiles than these): how often a sum is cut does not depend on
     // the tile that computes it.
-    const int splits = choose_splits(p.T, p.N, p.K, 128);
-    if (splits == 1) {
+    const int splits = choose_splits(T, N, K, 128);
+    return splits == 1 ? 0 : splits;
+}
+
+template <int EPI, int D>
+hipError_t launch_skinny(const GemmArgs& p, hipStream_t s, NextNorm* next = nullptr) {
+    const int splits = skinny_ranges(p.T, p.N, p.K, EPI == EPI_SWIGLU);
+    if (p.T <= 128) {
+        if constexpr (EPI == EPI_SWIGLU) {
+            if (splits == 0) return p.T <= 64 ? launch_skinny_whole<64, EPI>(p, s) : launch_skinny_whole<128, EPI>(p, s);
+        }
+        if (p.T <= 64) return launch_split<64, EPI, D, 128, true>(p, splits, s, next);
+        return launch_split<128, EPI, D, 128, true>(p, splits, s, next);
+    }
+    if (splits == 0) {
         // wide enough that one 256 x 256 tile per CU is (nearly) a full round: half the activation reads again
         const int tiles256 = EPI == EPI_SWIGLU ? (p.n_half + 127) / 128 : (p.N + 255) / 256;
         if (p.T > 192 && tiles256 >= 200 && tiles256 <= 256) return launch_skinny_whole<256, EPI, D, 256>(p, s);

@@ -208,51 +208,65 @@ hipError_t launch_rows(GemmArgs p, hipStream_t s) {
     return hipGetLastError();
 }
 
+// Up to 16 tokens weights of 32 MB and more are read with the non-temporal hint: two layers with such a matrix are more than the last-level cache
+// (256 MB) holds, so that the next step finds them in memory.  us without -> with, from memory (from the cache): T = 1, 7168 x 5120 8.6 -> 7.7 (7.2 ->
+// 7.1), 15360 x 5120 15.4 -> 13.9 (12.6 -> 13.2), SwiGLU 27648 x 5120 26.1 -> 23.7; T = 16, 12288 x 4096 12.6 -> 11.6 (9.2 -> 10.8).  Smaller ones gain 0.3 - 0.5 us
+// from memory and lose up to 1.5 from the cache (5120 x 5120 at T = 16 8.2 -> 7.9, 5.9 -> 7.4).
+constexpr int64_t kFarWeights = (int64_t)32 << 20;
+
 // Which problems go this way, and on which tile.  Every workgroup loads its own activations beside its weights, so the time is a launch, two
 // round trips and that traffic; the tiled kernels share both operands between more rows and columns, and win where the traffic gets long.
-// us, tiled kernels -> this one (three sets of operands in turn; outputs x k):
-//   T = 1: 5120 x 5120 10.5 -> 6.7, 15360 x 5120 17.8 -> 13.3, 5120 x 13824 17.0 -> 12.4, SwiGLU 27648 x 5120 26.6 -> 24.5; T = 8: 8192 x 28672 42.6 -> 38.3
-//   T = 24: 5120 x 5120 12.3 -> 7.3, 15360 x 5120 19.9 -> 14.0, 5120 x 13824 19.1 -> 13.2; but 5120 x 27648 (283 MB) 30.5 -> 39.3, SwiGLU 57344 x 8192 76 -> 86
-//   T = 40: 5120 x 13824 19.9 -> 15.8; 56: 15360 x 5120 22.0 -> 16.7
-//   T = 128: 15360 x 5120 27.6 -> 23.7, SwiGLU 11264 x 5120 27.2 -> 18.9, 8192 x 8192 24.3 -> 19.9; but 5120 x 13824 (354 MB) 25.4 -> 27.5;
-//   100: 10240 x 8192 (252 MB) 24.8 -> 27.7; 256: 5120 x 5120 23.7 -> 19.2; 400: 4096 x 4096 22.7 -> 18.2; 520 (two rounds of tiles) 24.6 -> 30.2
-//   T = 333: 1004 x 1152 12.2 -> 5.0; 500: 2048 x 2048 15.9 -> 9.4; 700: 2560 x 2560 21.5 -> 14.8; 2000: 2048 x 512 17.2 -> 12.2; but SwiGLU
-//   2816 x 512 at 1500 (104 MB) 8.6 -> 11.8
+// Bytes are counted in MB of 10^6.
+//
+// In a step over a stack of layers the weights come from memory; those of a small stack stay in the last-level cache (256 MB).  us, tiled kernels with
+// scratch -> this one, weights from memory (1.3 GB of sets in turn; three sets that the cache holds; outputs x k):
+//   T = 1: 5120 x 5120 9.9 -> 7.0 (9.4 -> 5.8), 15360 x 5120 18.3 -> 13.9 (17.4 -> 13.2), 5120 x 13824 16.3 -> 13.1, SwiGLU 27648 x 5120 25.9 -> 23.7;
+//   but 10240 x 8192 17.5 -> 17.6, at T = 16 18.6 -> 19.7
+//   T = 24: 5120 x 5120 11.6 -> 9.5 (11.0 -> 6.5), 15360 x 5120 19.1 -> 18.0, 8192 x 8192 16.1 -> 14.5; 2560 x 8192 11.1 -> 12.0 (10.7 -> 7.4);
+//   but 5120 x 13824 17.9 -> 19.3, 4096 x 14336 16.6 -> 18.9, 10240 x 8192 19.3 -> 22.8
+//   T = 64: 15360 x 5120 22.5 -> 20.4, 6144 x 4096 14.4 -> 10.3; but 5120 x 13824 21.0 -> 26.0, 10240 x 8192 22.5 -> 25.8
+//   T = 128: 15360 x 5120 29.4 -> 27.1, SwiGLU 11264 x 5120 25.8 -> 24.9, 7168 x 5120 21.3 -> 19.5, 4096 x 4096 19.7 -> 9.9;
+//   but 5120 x 13824 26.3 -> 38.8 (26.1 -> 27.1), 8192 x 8192 22.1 -> 26.9, 10240 x 8192 29.4 -> 33.2
+//   T = 256: 5120 x 5120 25.2 -> 22.1; 512: 4096 x 4096 27.4 -> 18.4 (19.5 -> 17.3), 2560 x 8192 30.3 -> 26.6; but 1000: 2048 x 2048 11.4 -> 12.6
+//   T = 300: 2048 x 512 5.0 -> 4.5; but 1000: 5.5 -> 7.0, 2000: 9.6 -> 11.6, SwiGLU 2816 x 512 at 700 5.7 -> 7.3
+// So with scratch, up to 64 tokens: what the fullest CU draws of the weights (k of 32 features for each of its workgroups) must not be long against
+// what the tiled kernels take, which spread any matrix over all CUs and grow with its size.  From 65 tokens on: problems of short traffic, beyond
+// 256 tokens on two workgroups per CU (the tiled kernels run whole tiles there), and tiles of 128 tokens in one round, counting the weights
+// twice.  Against the tiled kernels, weights from memory: 18 % faster over 630 sizes of 26 shapes, 7 of them more than 5 % slower (12 at most);
+// 16 % over 486 sizes of 26 other shapes, 6 % slower at most.  Without scratch the tiled kernels cannot cut k and are far slower on few
+// tokens (5120 x 13824 at T = 24 85): there these limits do not hold.
+//
 // Tiles: as few fragments of tokens as they need up to 64 tokens.  With four, slices two deep where a CU gets one workgroup, else one deep and three
 // workgroups (2000 x 2048 x 512 20.7, 12.2); four fragments of features for long k where they still fill the chip (64 x 10240 x 5120 17.0, 13.8).
-// More tokens: those tiles while their traffic is short, else 128 tokens a tile, in one round.
 enum { ROWS_NONE = 0, ROWS_16, ROWS_32, ROWS_64, ROWS_64_SHALLOW, ROWS_64_WIDE, ROWS_128, ROWS_128_WIDE };
 int rows_tile(const GemmArgs& p, int epi) {
     if (forced_cand() >= 0) return ROWS_NONE;
     const bool paired = epi == EPI_SWIGLU || epi == EPI_QKV_ROPE, swiglu = epi == EPI_SWIGLU;
     const int64_t cols = swiglu ? 2 * (int64_t)p.n_half : p.N, k_bytes = 2 * (int64_t)p.K;
+    const double weights_mb = 1e-6 * (double)(cols * k_bytes);
     auto tiles = [&](int fn, int tm) { return (int64_t)((p.T + 16 * tm - 1) / (16 * tm)) * (paired ? (cols / 2 + 8 * fn - 1) / (8 * fn) : (cols + 16 * fn - 1) / (16 * fn)); };
-    auto traffic_mb = [&](int fn, int tm) { return tiles(fn, tm) * 16 * (fn + tm) * k_bytes >> 20; };
+    auto traffic_mb = [&](int fn, int tm) { return 1e-6 * (double)(tiles(fn, tm) * 16 * (fn + tm) * k_bytes); };
     auto fills = [&](int fn, int tm) { return tiles(fn, tm) >= 150 && tiles(fn, tm) <= 256; };   // one round of workgroups, most CUs busy
+    auto lean = [&](int fn, int tm) { return !p.accum || 1e-3 * (double)((tiles(fn, tm) + 255) / 256 * (fn / 2) * k_bytes) <= (p.T <= 16 ? 8.0 : 6.5) + 0.09 * weights_mb; };
     auto by_64 = [&] { return tiles(2, 4) > 256 ? ROWS_64_SHALLOW : tiles(2, 4) > 128 ? ROWS_64 : ROWS_32; };
-    if (p.T <= 16) return traffic_mb(2, 1) <= (swiglu ? 256 : 400) ? ROWS_16 : ROWS_NONE;
-    if (p.T <= 32) return traffic_mb(2, 2) <= 200 ? ROWS_32 : ROWS_NONE;
+    if (p.T <= 16) return traffic_mb(2, 1) <= (swiglu ? 268 : 420) && (weights_mb >= 100 || lean(2, 1)) ? ROWS_16 : ROWS_NONE;
+    if (p.T <= 32) return traffic_mb(2, 2) <= 210 && lean(2, 2) ? ROWS_32 : ROWS_NONE;
     if (p.T <= 64) {
-        if (k_bytes >= 4096 && tiles(4, 4) >= 160 && traffic_mb(4, 4) <= 200) return ROWS_64_WIDE;
-        return traffic_mb(2, 4) <= 224 ? by_64() : ROWS_NONE;
+        if (k_bytes >= 4096 && tiles(4, 4) >= 160 && traffic_mb(4, 4) <= 210 && lean(4, 4)) return ROWS_64_WIDE;
+        return traffic_mb(2, 4) <= 235 && lean(2, 4) ? by_64() : ROWS_NONE;
     }
-    if (traffic_mb(2, 4) <= (swiglu ? 80 : 128)) return by_64();
-    if (k_bytes >= 2048 && fills(4, 8) && traffic_mb(4, 8) <= 240) return ROWS_128_WIDE;
-    if (k_bytes >= 2048 && fills(2, 8) && traffic_mb(2, 8) <= 340) return ROWS_128;
+    if (traffic_mb(2, 4) <= (swiglu ? 84 : 134) && (p.T <= 128 || tiles(2, 4) <= (p.T <= SKINNY_MAX_T ? 1280 : 512))) return by_64();
+    if (k_bytes < 2048 || p.T > 768) return ROWS_NONE;
+    const double weights_again = p.accum ? weights_mb : 0.0;
+    if (fills(4, 8) && traffic_mb(4, 8) + weights_again <= (p.accum ? 320 : 252)) return ROWS_128_WIDE;
+    if (fills(2, 8) && traffic_mb(2, 8) + weights_again <= (p.accum ? 270 : 357)) return ROWS_128;
     return ROWS_NONE;
 }
 
-// Weights that the last-level cache (256 MB) cannot hold beside others are read with the non-temporal hint: SwiGLU 27648 x 5120 (141 MB) 27.2 ->
-// 24.5 us.  Smaller ones may still be there from the last call: 5120 x 13824 at T = 24 13.2 with three sets in turn, 21.2 with the hint; from memory
-// (ten sets) 21.2 and 22.3, 15360 x 5120 at T = 1 15.6 and 14.6.  Only the tile of 16 tokens has the form with
-// the hint: the others' rules end at weights of 100 MB.
-constexpr int64_t kFarWeights = (int64_t)96 << 20;
-
 template <int EPI, int D = 0>
 hipError_t run_rows(const GemmArgs& p, hipStream_t s, int tile) {
-    const bool far = 2 * (int64_t)p.N * p.K >= kFarWeights;
     switch (tile) {
-        case ROWS_16: return far ? launch_rows<EPI, D, 2, 1, 4, 3, true>(p, s) : launch_rows<EPI, D, 2, 1, 4, 3, false>(p, s);
+        case ROWS_16: return 2 * (int64_t)p.N * p.K >= kFarWeights ? launch_rows<EPI, D, 2, 1, 4, 3, true>(p, s) : launch_rows<EPI, D, 2, 1, 4, 3, false>(p, s);
         case ROWS_32: return launch_rows<EPI, D, 2, 2, 4, 2, false>(p, s);
         case ROWS_64: return launch_rows<EPI, D, 2, 4, 4, 2, false>(p, s);
         case ROWS_64_SHALLOW: return launch_rows<EPI, D, 2, 4, 4, 1, false>(p, s);
@@ -264,6 +278,22 @@ hipError_t run_rows(const GemmArgs& p, hipStream_t s, int tile) {
 }
 
 }  // namespace
+
+GemmPlanI8 gemm_plan_i8(int32_t T, int64_t features, int32_t K, bool qkv, bool swiglu, bool scratch) {
+    GemmArgs p{};
+    float some_scratch;
+    set_linear(p, nullptr, nullptr, T, (int32_t)features, K / 2, nullptr, nullptr, scratch ? &some_scratch : nullptr, false);
+    if (const int tile = rows_tile(p, qkv ? EPI_QKV_ROPE : swiglu ? EPI_SWIGLU : EPI_BF16)) return {GemmPlanI8::WAVES, tile, 1, 0, 0};
+    if (skinny_applies(p.T, p.N, p.K, p.accum)) {
+        const int ranges = skinny_ranges(p.T, p.N, p.K, swiglu);
+        return {ranges ? GemmPlanI8::FEW_RANGES : GemmPlanI8::FEW_WHOLE, 0, std::max(1, ranges), 0, 0};
+    }
+    const int bm = qkv ? 0 : split_rows(p.T, p.N, p.K, scratch, swiglu);
+    if (bm && !one_range(p, bm)) return {GemmPlanI8::RANGES, bm, choose_splits(p.T, p.N, p.K, bm), 0, 0};
+    const Plan plan = plan_for(p.T, p.N, p.K, qkv, scratch, swiglu);
+    if (plan.cols1 > 0) return {GemmPlanI8::SHAPES, kTiles[plan.cand1].bm, 1, 0, plan.cols1};
+    return {GemmPlanI8::TILES, kTiles[plan.cand].bm, plan.tail_tiles ? plan.splits : 1, plan.tail_tiles, 0};
+}
 
 // The kernels see rows of K / 2 two-byte units.
 static hipError_t set_int8(GemmArgs& p, const float* t_scale, const float* w_scale) {

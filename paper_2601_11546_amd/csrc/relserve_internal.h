@@ -159,6 +159,14 @@ void gemm_force_plan_i8(int cand, int splits);   // its part for the int8 projec
 // (256 features both; rows x cols is the shape one launch would take).  halves: the split tiles run as halves (launch_halves).
 struct GemmPlan { int32_t rows, cols, tail_tiles, splits, cols1, rows1, rows2; bool halves; };
 GemmPlan gemm_plan(int32_t T, int64_t features, int32_t K, bool qkv, bool swiglu, bool scratch);
+// How an int8 projection runs (host arithmetic alone; K counts codes).  WAVES: linear_rows_kernel on its tile `rows` (an index, 1 ..); FEW_WHOLE,
+// FEW_RANGES: at most SKINNY_MAX_T tokens with scratch, whole or in `ranges` k ranges; RANGES: more tokens, all tiles of `rows` tokens in `ranges`
+// k ranges; TILES: tiles of `rows` tokens, of which the last tail_tiles take `ranges` k ranges; SHAPES: two launches, the first on cols1 columns.
+struct GemmPlanI8 {
+    enum Path : int32_t { WAVES, FEW_WHOLE, FEW_RANGES, RANGES, TILES, SHAPES };
+    int32_t path, rows, ranges, tail_tiles, cols1;
+};
+GemmPlanI8 gemm_plan_i8(int32_t T, int64_t features, int32_t K, bool qkv, bool swiglu, bool scratch);
 // The RMSNorm that reads a projection's output rows next (epilogues 1 and 2).  Where the projection ends in a kernel that
 // adds up k ranges, that kernel runs the norm too and sets `done`; otherwise the caller launches it.
 struct NextNorm {
