@@ -1765,11 +1765,12 @@ int split_rows(int T, int N, int K, bool has_accum, bool swiglu) {
     if (!has_accum || T <= SKINNY_MAX_T || K % 64 || N % 4 || forced_cand() >= 0) return 0;
 #if RELSERVE_GEMM_INT8
     return split_rows_i8(T, N, K, swiglu);
-#endif
+#else
     const int tn = (N + 255) / 256;
     if (((T + 127) / 128) * tn <= 128) return 128;
     if (((T + 255) / 256) * tn <= 85 && K >= 8192) return 256;
     return 0;
+#endif
 }
 
 // k too short to cut (below 512): one k range leaves the sums of whole tiles, and the fused epilogue the bits of the finish kernel
@@ -1942,6 +1943,7 @@ double tile_sec(const TileCand& c, int K, double eff) { return 2.0 * c.bm * c.bn
 // the small ones are bound by L2 traffic and gain nothing
 double idle_boost(int64_t tiles, int64_t slots) { return tiles < slots ? 1.0 + 0.25 * (1.0 - (double)tiles / (double)slots) : 1.0; }
 
+#if !RELSERVE_GEMM_INT8
 // need_bn256: the fused q/k/v epilogue's tiles only
 Plan choose_cut(int T, int64_t n_eff, int K, bool need_bn256, bool allow_tail) {
     Plan best{0, 0, 1};
@@ -1970,6 +1972,7 @@ Plan choose_cut(int T, int64_t n_eff, int K, bool need_bn256, bool allow_tail) {
     }
     return best;
 }
+#endif
 
 // The cost of a round is the tile's MFMA work over the shape's in-tile efficiency (relative to 256 x 256) plus kRoundSec;
 // this trades tile quantisation in T (padding to BM), the incomplete round, and the efficiency against each other.
@@ -2071,10 +2074,11 @@ void two_shapes(int T, int64_t n_eff, int K, bool swiglu, Plan* plan, double pla
     auto cost = [&](int cand, int c) {
 #if RELSERVE_GEMM_INT8
         return 1e-6 * whole_us_i8(cand, T, (int64_t)c * 256, K, swiglu);
-#endif
+#else
         const TileCand& t = kTiles[cand];
         const int64_t tiles = (int64_t)((T + t.bm - 1) / t.bm) * c, rounds = (tiles + 255) / 256;
         return (double)rounds * (tile_sec(t, K, swiglu ? t.eff_swiglu : t.eff) + kRoundSec) / (t.bm >= 256 ? idle_boost(tiles, 256) : 1.0);
+#endif
     };
     if (!kInt8 && !kTiles[plan->cand].qkv) return;
     double best = kInt8 ? 1e-6 * plan_us * 0.97 : cost(plan->cand, cols) * (1.0 - kTwoShapesGain) - kSecondLaunchSec;
@@ -2116,11 +2120,11 @@ Plan plan_for(int T, int64_t n_eff, int K, bool need_bn256, bool allow_tail, boo
     double us;
     plan = plan_i8(T, n_eff, K, need_bn256, allow_tail, swiglu, &us);
     two_shapes(T, n_eff, K, swiglu, &plan, us);
-    return plan;
-#endif
+#else
     plan = choose_cut(T, n_eff, K, need_bn256, allow_tail);
     if (plan.tail_tiles == 0 && !(swiglu && K < swiglu_fit_k(T))) plan.cand = whole_tile(T, n_eff, K, need_bn256, swiglu);
     if (plan.tail_tiles == 0 && K % 64 == 0) two_shapes(T, n_eff, K, swiglu, &plan);   // (the kernel for other k knows no columns)
+#endif
     return plan;
 }
 
