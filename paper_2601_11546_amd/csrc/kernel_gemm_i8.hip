@@ -1,4 +1,4 @@
-// int8 projections: out[t, n] = sum_k a[t, k] w[n, k] * (w_scale[n] * a_scale[t]) of 8-bit integers, summed exactly in 32 bits: the kernels of
+// int8 projections: out[t, n] = sum_k a[t, k] w[n, k] * w_scale[n] * a_scale[t] of 8-bit integers, summed exactly in 32 bits: the kernels of
 // gemm_kernels.h on integers, with a factor for each token beside each feature's in their epilogues.
 #define RELSERVE_GEMM_INT8 1
 #include "gemm_kernels.h"

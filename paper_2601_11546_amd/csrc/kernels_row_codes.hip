@@ -228,7 +228,7 @@ __global__ void __launch_bounds__(TPR < 256 ? 256 : TPR) row_codes_kernel(RowCod
 }
 
 // Threads per row.  A row's chunks go to as few threads as hold them in three registers' worth each (more threads: more of them idle at the
-// end of a row; more chunks a thread: a longer chain of conversions per wave), us:
+// end of a row; more chunks a thread: a longer chain of conversions per wave), us, here and below with codes of two instructions less than now (above):
 //   rmsnorm 8192 x 5120 bf16     256 x 3: 23.2   64 x 10: 25.4   512 x 2: 27.5   1024 x 1: 37.7
 //   add + norm 8192 x 8192       512 x 2: 80.5   256 x 4: 83.2   1024 x 1: 82.3
 //   rows 1282 x 13824            512 x 4: 9.1    256 x 7: 8.9    1024 x 2: 9.1;    4099 x 28672   1024 x 4: 62.1   512 x 7: 63.2   read twice: 96
