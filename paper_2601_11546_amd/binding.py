@@ -476,7 +476,8 @@ def relserve_linear_i8_workspace_bytes(tokens: int, n: int) -> int:
 
 def relserve_linear_i8(a, a_scale, w, w_scale, epilogue: int, residual, out, n: int = 0, workspace=None, stream=None) -> None:
     """a [T, K], w [N, K] int8 codes (n > 0: w is packed by pack_codes and has n rows), a_scale [T], w_scale [N] fp32.
-    residual: bf16 (epilogue 1, or None) or fp32 (2); the others add none, and take None.  workspace: uint8 tensor of relserve_linear_i8_workspace_bytes(T, N) bytes or more, or None."""
+    residual: bf16 (epilogue 1, or None) or fp32 (2); the others add none, and take None.
+    workspace: uint8 tensor of relserve_linear_i8_workspace_bytes(T, N) bytes or more, or None."""
     t, k = shape = a.shape
     rows = n if n else w.shape[0]
     if residual is not None and epilogue in (0, 3):

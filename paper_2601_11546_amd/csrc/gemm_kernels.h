@@ -1685,7 +1685,7 @@ hipError_t launch_skinny_whole(GemmArgs p, hipStream_t s) {
     return of_operands(p, go);
 }
 
-// k ranges of such a projection, the ways the sums are cut; 0: whole tiles that fill the CUs.
+// k ranges of a projection of at most SKINNY_MAX_T tokens with scratch; 0: whole tiles, which fill the CUs.
 int skinny_ranges(int T, int N, int K, bool swiglu) {
     if (T <= 128) {
         // One token tile: the MFMA work is small next to the weight stream, so 128-feature tiles cost nothing
