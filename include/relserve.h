@@ -297,6 +297,22 @@ int32_t relserve_model_step_i8(const relserve_layer* layer, const relserve_batch
  * int32 [n_rows].  Integer result, defined exactly. */
 int32_t relserve_greedy_sample(const void* logits, int32_t n_rows, int32_t vocab, int32_t* next_token, void* stream);
 
+/* How sure the model is of an answer: of each row of logits the log probabilities of given tokens, the entropy and the most probable alternatives.
+ * With p = softmax of the row's vocab entries: logprobs[r, j] = log p[ids[r, j]] (NaN where the id is outside [0, vocab)), entropy[r] = - sum p log p in
+ * natural logarithms, top_ids[r, 0 .. n_top) the entries with the largest logits in falling order, the lowest id first among equal ones, and
+ * top_logprobs their log p.  Entries of -infinity have probability 0; a row with a NaN or an infinity, or with no entry above -infinity, has NaN for its
+ * log probabilities and entropy, while its alternatives are ordered all the same; NaN entries are no alternatives; behind the last entry of a row stand
+ * id -1 and -infinity.  Sums in fp32, their largest term held apart, so that a log probability next to 0 keeps its digits.
+ * logits: device, fp32 (logits_are_f32 != 0) or bf16, row r begins at element r * pitch (pitch >= vocab: columns behind the vocabulary are not read).
+ * ids [n_rows, n_ids], logprobs [n_rows, n_ids] fp32, entropy [n_rows] fp32 (or NULL), top_ids [n_rows, n_top], top_logprobs [n_rows, n_top] fp32; n_ids
+ * and n_top may be 0 (with NULL arrays), n_top at most 32.  n_rows at most 2^22, vocab 2^24 (RELSERVE_ERR_TOO_LARGE).  workspace: scratch as in
+ * relserve_layer_step, of at least relserve_logprobs_workspace_bytes bytes: a few rows are cut into parts for several workgroups.  With NULL they are not
+ * cut: last bits may differ, and few rows take longer. */
+int32_t relserve_logprobs_workspace_bytes(int32_t n_rows, int32_t vocab, int32_t n_top, size_t* out);
+int32_t relserve_logprobs(const void* logits, int32_t logits_are_f32, int32_t n_rows, int32_t vocab, int64_t pitch, const int32_t* ids,
+                          int32_t n_ids, float* logprobs, float* entropy, int32_t n_top, int32_t* top_ids, float* top_logprobs,
+                          void* workspace, size_t workspace_bytes, void* stream);
+
 /* ---- single stages, exported so that each kernel can be checked alone ---- */
 
 /* out[t, :] = x[t, :] * w / sqrt(mean(x[t, :]^2) + eps); x is bf16 when
@@ -378,6 +394,38 @@ typedef struct relserve_layer_weights_i8 {
 } relserve_layer_weights_i8;
 int32_t relserve_layer_step_i8(const relserve_layer* layer, const relserve_batch* batch, const relserve_layer_weights_i8* weights,
                                const void* x, void* y, relserve_kv_cache cache, void* workspace, size_t workspace_bytes, void* stream);
+
+/* ---- projections in 8-bit floating point with a scale for each block of 128 (a variant beside the paper's 16-bit models: the form in which
+ * checkpoints with 8-bit weights are commonly kept; nothing calibrated) ----
+ * Codes are those of relserve_layer_weights_w8a8 (1 sign, 4 exponent, 3 mantissa bits, bias 7, largest magnitude 448).  A weight matrix [N, K] has one
+ * fp32 scale for each block of 128 rows x 128 values, w_scale [ceil(N / 128), K / 128]; activations [T, K] have one for each 128 values of a token,
+ * which lie block by block, a_scale [K / 128, T].  A code stands for its value times its block's scale.  Scales may be any fp32 numbers; those that the calls
+ * below make are
+ *     scale = m / 448, m the block's largest magnitude;  code = the number of the format nearest to value * 448 / m (ties to even).
+ * Codes of bf16 matrices are exactly these, and so are those of norms of bf16 streams, with s * w as the value, since the norm's factor cancels; a norm of
+ * an fp32 stream rounds s * w and the quotient to fp32 first.  A block of zeros has scale 0; one with a NaN or an infinity has a scale that is not finite
+ * and codes of 0: whatever is computed from it is not finite either.
+ * All pointers are device memory, 16-byte aligned but for scales (RELSERVE_ERR_BAD_ARGUMENT otherwise).
+ *
+ * relserve_quantise_f8b: codes and scales of in [n_rows, n] bf16 in blocks of block_rows x 128; n a multiple of 128, at most 2^22, n_rows at most 2^30
+ * here and below (RELSERVE_ERR_TOO_LARGE).  block_rows = 1: activations, scales [n / 128, n_rows]; 128: weights, scales [ceil(n_rows / 128), n / 128].
+ *
+ * relserve_add_rmsnorm_f8b: relserve_add_rmsnorm_i8 with these codes: s = x + delta, rounded to x's type, kept in sum if given (which may be x, and overlaps
+ * nothing else); codes and scales [hidden / 128, n_rows] of s * w / sqrt(mean(s^2) + eps).
+ *
+ * relserve_linear_f8b: out[t, n] = sum over blocks b of k of (sum over k in b of a[t, k] * w[n, k]) * (a_scale[b, t] * w_scale[n / 128, b]) on codes: a block's
+ * products exact, its sum in fp32, added with one fused multiply-add; epilogues, residuals and outputs as relserve_linear (0 and 3 read no residual).
+ * K a multiple of 128, N of 4 (of 16 for SwiGLU).  With SwiGLU the gate's and the up's rows are blocked each from their own first one: w_scale
+ * [2 ceil(N / 256), K / 128].  packed != 0: w is relserve_pack_weight applied to the matrix seen as [N, K / 2] two-byte units.  workspace: scratch
+ * as in relserve_layer_step, of at least relserve_linear_f8b_workspace_bytes(T, N) bytes: holds partial sums where k is cut into ranges for several
+ * workgroups.  With NULL k is never cut: last bits may differ, and few tokens or outputs on long k take longer. */
+int32_t relserve_quantise_f8b(const void* in, int32_t n_rows, int32_t n, int32_t block_rows, void* codes, float* scales, void* stream);
+int32_t relserve_add_rmsnorm_f8b(const void* x, int32_t x_is_f32, const void* delta, const void* w, float eps, int32_t n_rows,
+                                 int32_t hidden, void* sum, void* codes, float* scales, void* stream);
+int32_t relserve_linear_f8b_workspace_bytes(int32_t T, int32_t N, size_t* out);
+int32_t relserve_linear_f8b(const void* a, const float* a_scale, const void* w, const float* w_scale, int32_t T, int32_t N, int32_t K,
+                            int32_t epilogue, const void* residual, void* out, int32_t packed, void* workspace, size_t workspace_bytes,
+                            void* stream);
 
 /* out[T, N] = a[T, K] * w[N, K]^T (Eq. 3 and every other dense map), bf16 in,
  * fp32 accumulate.  epilogue: 0 = store bf16; 1 = add residual (bf16 [T, N],

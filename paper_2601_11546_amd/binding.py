@@ -40,7 +40,9 @@ EXPORTS = ["relserve_version", "relserve_strerror", "relserve_config_validate", 
            "relserve_priority_reuse", "relserve_prefill_candidate",
            "relserve_layer_step_w8a8", "relserve_model_step_w8a8", "relserve_rmsnorm_codes", "relserve_quantise_bf16", "relserve_linear_w8a8",
            "relserve_quantise_rows_i8", "relserve_add_rmsnorm_i8", "relserve_linear_i8", "relserve_linear_i8_workspace_bytes",
-           "relserve_qkv_rope_append_i8", "relserve_layer_step_i8", "relserve_model_step_i8"]
+           "relserve_qkv_rope_append_i8", "relserve_layer_step_i8", "relserve_model_step_i8",
+           "relserve_quantise_f8b", "relserve_add_rmsnorm_f8b", "relserve_linear_f8b", "relserve_linear_f8b_workspace_bytes",
+           "relserve_logprobs", "relserve_logprobs_workspace_bytes"]
 
 
 class RelserveError(RuntimeError):
@@ -159,6 +161,15 @@ for _n, _a in {
     "relserve_qkv_rope_append_i8": [C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, KVCache, C.c_int32,
                                     C.c_void_p, C.c_size_t, C.c_void_p],
     "relserve_layer_step_i8": [C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, KVCache, C.c_void_p, C.c_size_t, C.c_void_p],
+    "relserve_quantise_f8b": [C.c_void_p, C.c_int32, C.c_int32, C.c_int32, C.c_void_p, C.c_void_p, C.c_void_p],
+    "relserve_add_rmsnorm_f8b": [C.c_void_p, C.c_int32, C.c_void_p, C.c_void_p, C.c_float, C.c_int32, C.c_int32, C.c_void_p, C.c_void_p,
+                                 C.c_void_p, C.c_void_p],
+    "relserve_linear_f8b_workspace_bytes": [C.c_int32, C.c_int32, C.c_void_p],
+    "relserve_linear_f8b": [C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_int32, C.c_int32, C.c_int32, C.c_int32, C.c_void_p,
+                            C.c_void_p, C.c_int32, C.c_void_p, C.c_size_t, C.c_void_p],
+    "relserve_logprobs_workspace_bytes": [C.c_int32, C.c_int32, C.c_int32, C.c_void_p],
+    "relserve_logprobs": [C.c_void_p, C.c_int32, C.c_int32, C.c_int32, C.c_int64, C.c_void_p, C.c_int32, C.c_void_p, C.c_void_p, C.c_int32,
+                          C.c_void_p, C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p],
     "relserve_model_workspace_bytes": [C.c_void_p, C.c_int32, C.c_int32, C.c_void_p],
     "relserve_model_step": [C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_size_t,
                             C.c_void_p],
@@ -538,6 +549,84 @@ def relserve_layer_step_i8(layer, pbatch, weights: dict, x, y, k_pages, v_pages,
     _check(_lib.relserve_layer_step_i8(layer.handle, pbatch.handle, C.byref(wt), x.data_ptr(), y.data_ptr(), _cache(k_pages, v_pages),
                                        workspace.data_ptr(), workspace.numel() * workspace.element_size(), _stream_address(x, stream)),
            "relserve_layer_step_i8")
+
+
+def _codes_dtype(t):
+    """What _dense expects of 8-bit floating point codes: bytes, or torch's type of the format."""
+    return torch.float8_e4m3fn if t.dtype is torch.float8_e4m3fn else torch.uint8
+
+
+def relserve_quantise_f8b(values, codes, scales, block_rows: int = 1, stream=None) -> None:
+    """codes [T, n] (uint8 or float8_e4m3fn) of values [T, n] bf16 in blocks of 1 x 128, scales [n / 128, T] fp32, or of 128 x 128,
+    scales [ceil(T / 128), n / 128]."""
+    rows, n = shape = values.shape
+    _dense("relserve_quantise_f8b", ("values", values, torch.bfloat16, shape), ("codes", codes, _codes_dtype(codes), shape),
+           ("scales", scales, torch.float32, ((rows + 127) // 128, n // 128) if block_rows == 128 else (n // 128, rows)))
+    _check(_lib.relserve_quantise_f8b(values.data_ptr(), rows, n, block_rows, codes.data_ptr(), scales.data_ptr(), _stream_address(values, stream)),
+           "relserve_quantise_f8b")
+
+
+def relserve_add_rmsnorm_f8b(x, w, eps: float, codes, scales, delta=None, sum_out=None, stream=None) -> None:
+    """codes [T, H], scales [H / 128, T] fp32 of the normed x + delta (x bf16 or fp32, delta bf16); sum_out (may be x): x + delta."""
+    rows, n = shape = x.shape
+    f32 = x.dtype is torch.float32
+    dtype = torch.float32 if f32 else torch.bfloat16
+    _dense("relserve_add_rmsnorm_f8b", ("x", x, dtype, shape), ("w", w, torch.bfloat16, (n,)), ("codes", codes, _codes_dtype(codes), shape),
+           ("scales", scales, torch.float32, (n // 128, rows)), ("delta", delta, torch.bfloat16, shape), ("sum_out", sum_out, dtype, shape))
+    _check(_lib.relserve_add_rmsnorm_f8b(x.data_ptr(), f32, _address(delta), w.data_ptr(), eps, rows, n, _address(sum_out), codes.data_ptr(),
+                                         scales.data_ptr(), _stream_address(x, stream)), "relserve_add_rmsnorm_f8b")
+
+
+def relserve_linear_f8b_workspace_bytes(tokens: int, n: int) -> int:
+    out = C.c_size_t()
+    _check(_lib.relserve_linear_f8b_workspace_bytes(int(tokens), int(n), C.byref(out)), "relserve_linear_f8b_workspace_bytes")
+    return int(out.value)
+
+
+def relserve_linear_f8b(a, a_scale, w, w_scale, epilogue: int, residual, out, n: int = 0, workspace=None, stream=None) -> None:
+    """a [T, K], w [N, K] codes (uint8 or float8_e4m3fn; n > 0: w is packed by pack_codes and has n rows), a_scale [K / 128, T] fp32, w_scale fp32 by
+    blocks of 128 rows (with epilogue 3 of the gate's and then of the up's) x 128.  residual: bf16 (epilogue 1, or None) or fp32 (2); the others take None.
+    workspace: uint8 tensor of relserve_linear_f8b_workspace_bytes(T, N) bytes or more, or None."""
+    t, k = shape = a.shape
+    rows = n if n else w.shape[0]
+    if residual is not None and epilogue in (0, 3):
+        raise ValueError(f"relserve_linear_f8b: epilogue {epilogue} adds no residual")
+    blocks = 2 * ((rows // 2 + 127) // 128) if epilogue == 3 else (rows + 127) // 128
+    _dense("relserve_linear_f8b", ("a", a, _codes_dtype(a), shape), ("a_scale", a_scale, torch.float32, (k // 128, t)),
+           ("w", w, _codes_dtype(w), ((rows + 255) // 256 * 256 * k,) if n else (rows, k)), ("w_scale", w_scale, torch.float32, (blocks, k // 128)),
+           ("out", out, torch.float32 if epilogue == 1 else torch.bfloat16, (t, rows // 2 if epilogue == 3 else rows)),
+           ("residual", residual, torch.bfloat16 if epilogue == 1 else torch.float32, (t, rows)),
+           ("workspace", workspace, torch.uint8, workspace.shape if workspace is not None else ()))
+    _check(_lib.relserve_linear_f8b(a.data_ptr(), a_scale.data_ptr(), w.data_ptr(), w_scale.data_ptr(), t, rows, k, epilogue, _address(residual),
+                                    out.data_ptr(), n > 0, _address(workspace), 0 if workspace is None else workspace.numel(),
+                                    _stream_address(a, stream)), "relserve_linear_f8b")
+
+
+def relserve_logprobs_workspace_bytes(rows: int, vocab: int, n_top: int) -> int:
+    out = C.c_size_t()
+    _check(_lib.relserve_logprobs_workspace_bytes(int(rows), int(vocab), int(n_top), C.byref(out)), "relserve_logprobs_workspace_bytes")
+    return int(out.value)
+
+
+def relserve_logprobs(logits, ids=None, logprobs=None, entropy=None, top_ids=None, top_logprobs=None, workspace=None, stream=None) -> None:
+    """logits [rows, vocab] fp32 or bf16 (rows may be further apart: the first columns of a wider matrix); ids [rows, G] int32 and logprobs [rows, G]
+    fp32; entropy [rows] fp32; top_ids [rows, k] int32 and top_logprobs [rows, k] fp32.  workspace: uint8 tensor of relserve_logprobs_workspace_bytes
+    bytes or more, or None."""
+    rows, vocab = logits.shape
+    f32 = logits.dtype is torch.float32
+    if (logits.dtype is not torch.bfloat16 and not f32) or (vocab > 1 and logits.stride(1) != 1) or (rows > 1 and logits.stride(0) < vocab):
+        raise ValueError(f"relserve_logprobs: logits must be rows of fp32 or bf16 entries one behind the other, not {logits.dtype} with strides "
+                         f"{logits.stride()}")
+    if (ids is None) != (logprobs is None) or (top_ids is None) != (top_logprobs is None):
+        raise ValueError("relserve_logprobs: ids and logprobs, top_ids and top_logprobs are given together")
+    n_ids, n_top = 0 if ids is None else ids.shape[1], 0 if top_ids is None else top_ids.shape[1]
+    _dense("relserve_logprobs", ("logits", logits[:1, :1].reshape(-1) if rows else logits.reshape(-1), logits.dtype, (min(rows, 1),)),
+           ("ids", ids, torch.int32, (rows, n_ids)), ("logprobs", logprobs, torch.float32, (rows, n_ids)), ("entropy", entropy, torch.float32, (rows,)),
+           ("top_ids", top_ids, torch.int32, (rows, n_top)), ("top_logprobs", top_logprobs, torch.float32, (rows, n_top)),
+           ("workspace", workspace, torch.uint8, workspace.shape if workspace is not None else ()))
+    _check(_lib.relserve_logprobs(logits.data_ptr(), f32, rows, vocab, logits.stride(0) if rows > 1 else vocab, _address(ids), n_ids,
+                                  _address(logprobs), _address(entropy), n_top, _address(top_ids), _address(top_logprobs), _address(workspace),
+                                  0 if workspace is None else workspace.numel(), _stream_address(logits, stream)), "relserve_logprobs")
 
 
 def relserve_static_scratch_bytes() -> int:

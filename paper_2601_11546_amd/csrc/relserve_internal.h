@@ -212,6 +212,32 @@ hipError_t launch_linear_i8(const void* a, const float* a_scale, const void* w, 
 hipError_t launch_qkv_rope_append_i8(const BatchDev& b, const relserve_layer& L, const void* h, const float* h_scale, const void* w_qkv,
                                      const float* w_scale, void* q_out, void* k_pages, void* v_pages, hipStream_t s, float* accum,
                                      bool w_packed, KvFormat kv);
+// A matrix as 8-bit floating point codes with a scale for each block of block_rows (1 or 128) x 128; scales [n / 128, rows] or [rows / 128, n / 128]
+hipError_t launch_block_codes(const void* in, int32_t rows, int32_t n, int32_t block_rows, void* codes, float* scales, hipStream_t s);
+// The same of rmsnorm(x + delta) * w in blocks of 1 x 128 (delta may be null; sum, if given, receives x + delta in x's type)
+hipError_t launch_add_rmsnorm_f8b(const void* x, bool x_is_f32, const void* delta, const void* w, float eps, int32_t rows, int32_t n, void* sum,
+                                  void* codes, float* scales, hipStream_t s);
+// launch_linear on such codes: a [T, K] with a_scale [K / 128, T], w [N, K] with w_scale [blocks of 128 rows, K / 128].  scratch: null, or
+// gemm_f8b_scratch_floats(T, N) floats, contents irrelevant on entry: k is cut into ranges where that pays
+int64_t gemm_f8b_scratch_floats(int64_t T, int64_t N);
+hipError_t launch_linear_f8b(const void* a, const float* a_scale, const void* w, const float* w_scale, int32_t T, int32_t N, int32_t K,
+                             int32_t epilogue, const void* residual, void* out, hipStream_t s, float* scratch, bool w_packed);
+// Log probabilities of rows of logits (see relserve_logprobs); scratch: null, or logprobs_scratch_bytes(rows, vocab, n_top) bytes
+struct LogprobsArgs {
+    const void* logits;
+    int32_t is_f32, rows, vocab;
+    int64_t pitch;
+    const int32_t* ids;
+    int32_t n_ids;
+    float* logprobs;
+    float* entropy;
+    int32_t n_top;
+    int32_t* top_ids;
+    float* top_logprobs;
+    void* scratch;
+};
+int64_t logprobs_scratch_bytes(int64_t rows, int64_t vocab, int64_t n_top);
+hipError_t launch_logprobs(const LogprobsArgs& args, hipStream_t s);
 // bf16 [n] -> 8-bit codes of value / scale (n % 8 == 0)
 hipError_t launch_quantise_bf16(const void* in, int64_t n, float scale, void* codes, hipStream_t s);
 // Attention passes; part_o [T + split_slot_cap(T), n_q, d] fp32 and part_ml [.., n_q, 2] fp32 hold the prefix partials
