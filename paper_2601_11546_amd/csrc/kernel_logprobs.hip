@@ -4,10 +4,13 @@
 // Z = c + s and log Z = log1p((c - 1) + s), so that a nearly sure row keeps the digits of a log probability next to 0; both terms of H are
 // positive, so nothing cancels in it.
 //
-// A workgroup of 256 threads holds 8192 values of a row at a time, 32 a thread, all loaded at once.  Its alternatives are kept as 64-bit keys,
-// the value's bits in an order of whole numbers above the id's complement: larger value first, the lower id among equals, all keys different.
-// Of a chunk only the values that can be among the first n_top are looked at: those from the n_top-th largest of its 256 threads' best on (found among
-// the groups of four lanes first), so at most 32 n_top of them, whatever the row.
+// A workgroup of 256 threads holds 8192 values of a row at a time, 32 a thread, while the next ones are on their way.  Nothing in that pass waits for
+// another thread; a thread remembers its largest value and the chunk it came in.
+//
+// Alternatives are 64-bit keys, the value's bits in an order of whole numbers above the id's complement: larger value first, the lower id among
+// equals, all keys different.  Behind the pass the largest values of the groups of four lanes give a bound that n_top values reach at least; the
+// loads of the threads whose largest value reaches it are dealt out to all threads once more (from the caches), and what reaches the bound is
+// gathered and ranked.  Where ties let too much reach it, the bound is the n_top-th of the 256 threads' best keys.
 //
 // Few rows are cut into parts of whole chunks for several workgroups, whose results a second launch joins in their order.
 #include <algorithm>
@@ -29,18 +32,13 @@ struct Sums {
 // What a sum of smaller values counts for at m: nothing if it holds none, a NaN if it holds one.
 __device__ __forceinline__ void move_to(Sums& a, float m) {
     if (a.m == m) return;
-    const float all = a.m == -INFINITY ? (a.s != a.s ? a.s : 0.0f) : a.c + a.s, d = a.m == -INFINITY ? 0.0f : a.m - m;
-    const float f = a.m == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(d * LOG2E);
-    a.e = (a.m == -INFINITY ? 0.0f : __builtin_fmaf(fmaxf(d, -200.0f), all, a.e)) * f;
+    const bool none = a.m == -INFINITY;
+    const float all = none ? (a.s != a.s ? a.s : 0.0f) : a.c + a.s, d = none ? 0.0f : a.m - m;
+    const float f = none ? 0.0f : __builtin_amdgcn_exp2f(d * LOG2E);
+    a.e = (none ? 0.0f : __builtin_fmaf(fmaxf(d, -200.0f), all, a.e)) * f;
     a.s = all * f;
     a.c = 0.0f;
     a.m = m;
-}
-__device__ __forceinline__ Sums joined(Sums a, Sums b) {
-    const float m = fmaxf(a.m, b.m);
-    move_to(a, m);
-    move_to(b, m);
-    return {m, a.c + b.c, a.s + b.s, a.e + b.e};
 }
 // log Z; a row with a NaN, an infinity or no finite value has no distribution
 __device__ __forceinline__ float log_z(const Sums& a) { return a.m > -INFINITY && a.m < INFINITY ? log1pf((a.c - 1.0f) + a.s) : NAN; }
@@ -59,20 +57,27 @@ struct LogprobsLaunch {
     uint64_t* part_keys;     // [rows, parts, n_top]
 };
 
+__device__ __forceinline__ float logit(const LogprobsArgs& a, int64_t at) {
+    return a.is_f32 ? static_cast<const float*>(a.logits)[at] : bf16_to_f32(static_cast<const uint16_t*>(a.logits)[at]);
+}
+
+// The logit of the row's given token that this thread answers for first (fetched ahead of what it waits for).
+struct Given { float x; bool valid; };
+__device__ __forceinline__ Given given(const LogprobsArgs& a, int64_t row, int j) {
+    if (j >= a.n_ids) return {0.0f, false};
+    const int32_t id = a.ids[row * a.n_ids + j];
+    const bool valid = id >= 0 && id < a.vocab;
+    return {valid ? logit(a, row * a.pitch + id) : 0.0f, valid};
+}
+
 // What is left to do when a row's sums and keys are known.
-__device__ __forceinline__ void write_row(const LogprobsArgs& a, int64_t row, const Sums& z, const uint64_t* keys) {
+__device__ __forceinline__ void write_row(const LogprobsArgs& a, int64_t row, const Sums& z, const uint64_t* keys, Given first) {
     const float lz = log_z(z);
     const int tid = threadIdx.x;
     if (tid == 0 && a.entropy) a.entropy[row] = lz - z.e / (z.c + z.s);
     for (int j = tid; j < a.n_ids; j += THREADS) {
-        const int32_t id = a.ids[row * a.n_ids + j];
-        float lp = NAN;
-        if (id >= 0 && id < a.vocab) {
-            const int64_t at = row * a.pitch + id;
-            const float x = a.is_f32 ? static_cast<const float*>(a.logits)[at] : bf16_to_f32(static_cast<const uint16_t*>(a.logits)[at]);
-            lp = (x - z.m) - lz;
-        }
-        a.logprobs[row * a.n_ids + j] = lp;
+        const Given v = j == tid ? first : given(a, row, j);
+        a.logprobs[row * a.n_ids + j] = v.valid ? (v.x - z.m) - lz : NAN;
     }
     if (tid < a.n_top) {
         const uint64_t k = keys[tid];
@@ -81,138 +86,275 @@ __device__ __forceinline__ void write_row(const LogprobsArgs& a, int64_t row, co
     }
 }
 
-// The sums of all threads, in every thread.
-__device__ __forceinline__ Sums all_sums(Sums z, Sums* red) {
+// The sums of all threads, in every thread: moved to the largest value of all, then added.
+__device__ __forceinline__ Sums all_sums(Sums z, float4* red) {
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    float m = z.m;
 #pragma unroll
-    for (int o = 32; o > 0; o >>= 1) z = joined(z, Sums{__shfl_xor(z.m, o, 64), __shfl_xor(z.c, o, 64), __shfl_xor(z.s, o, 64), __shfl_xor(z.e, o, 64)});
-    if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = z;
-    __syncthreads();
-    z = red[0];
+    for (int o = 32; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor(m, o, 64));
+    move_to(z, m);
 #pragma unroll
-    for (int w = 1; w < THREADS / 64; ++w) z = joined(z, red[w]);
-    return z;
-}
-
-// The n largest of the keys in cand[0 .. count), in order, to list[0 .. n) (zeros behind them); all keys are different.
-__device__ __forceinline__ void largest_keys(const uint64_t* cand, int count, uint64_t* list, int n) {
-    for (int i = threadIdx.x; i < count; i += THREADS) {
-        const uint64_t k = cand[i];
-        int rank = 0;
-        for (int j = 0; j < count; ++j) rank += cand[j] > k;
-        if (rank < n) list[rank] = k;
+    for (int o = 32; o > 0; o >>= 1) {
+        z.c += __shfl_xor(z.c, o, 64);
+        z.s += __shfl_xor(z.s, o, 64);
+        z.e += __shfl_xor(z.e, o, 64);
     }
+    if (lane == 0) red[wave] = make_float4(z.m, z.c, z.s, z.e);
+    __syncthreads();
+    Sums part[THREADS / 64];
+    m = -INFINITY;
+#pragma unroll
+    for (int w = 0; w < THREADS / 64; ++w) {
+        const float4 r = red[w];
+        part[w] = {r.x, r.y, r.z, r.w};
+        m = fmaxf(m, r.x);
+    }
+    Sums all{m, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int w = 0; w < THREADS / 64; ++w) {
+        move_to(part[w], m);
+        all.c += part[w].c;
+        all.s += part[w].s;
+        all.e += part[w].e;
+    }
+    return all;
 }
 
-template <bool F32, bool TOP>
+// How many of keys[0 .. count) are larger than k; zeros stand behind the last one up to a multiple of eight.
+__device__ __forceinline__ int larger_keys(const uint64_t* keys, int count, uint64_t k) {
+    int rank = 0;
+    for (int j = 0; j < count; j += 8) {
+#pragma unroll
+        for (int q = 0; q < 8; ++q) rank += keys[j + q] > k;
+    }
+    return rank;
+}
+
+// 128 bits moved down by `bits`, with copies of fill behind them.
+__device__ __forceinline__ uint4 behind(const uint4& q, int bits, uint32_t fill) {
+    const uint64_t lo = (uint64_t)q.y << 32 | q.x, hi = (uint64_t)q.w << 32 | q.z, f = (uint64_t)fill << 32 | fill;
+    const int b = bits & 63;
+    const uint64_t a = bits < 64 ? lo : bits < 128 ? hi : f, c = bits < 64 ? hi : f;   // what lies b bits below the result
+    const uint64_t x = b ? a >> b | c << (64 - b) : a, y = b ? c >> b | f << (64 - b) : c;
+    return make_uint4((uint32_t)x, (uint32_t)(x >> 32), (uint32_t)y, (uint32_t)(y >> 32));
+}
+
+constexpr int kGathered = 2048;   // keys that a workgroup gathers at most: two chunks' of 32 alternatives
+
+template <bool F32, bool TOP, bool ONE>
 __global__ void __launch_bounds__(THREADS) logprobs_kernel(LogprobsLaunch p) {
     constexpr int V = F32 ? 4 : 8, LOADS = PER / V;   // values of a load
     typedef float f32_quad __attribute__((ext_vector_type(4), aligned(4)));
     typedef uint16_t bf16_eight __attribute__((ext_vector_type(8), aligned(2)));
-    __shared__ Sums red[THREADS / 64];
-    __shared__ uint64_t list[TOP ? MAX_TOP : 1], best[TOP ? THREADS : 1], cand[TOP ? MAX_TOP * (PER + 1) : 1], floor_key;
+    __shared__ float4 red[THREADS / 64];
+    __shared__ uint64_t list[TOP ? MAX_TOP : 1], best[TOP ? THREADS + 8 : 1], cand[TOP ? kGathered + MAX_TOP + 8 : 1], floor_key;
     __shared__ uint32_t group[TOP ? 64 : 1];
-    __shared__ int n_best, n_cand;
+    __shared__ uint8_t who[TOP && !ONE ? THREADS : 1];
+    __shared__ int n_best, n_cand, n_who;
     const int tid = threadIdx.x, lane = tid & 63, vocab = p.a.vocab, n_top = p.a.n_top;
     const int64_t row = blockIdx.x / p.parts;
-    const int part = blockIdx.x % p.parts, c0 = (int)((int64_t)p.chunks * part / p.parts), c1 = (int)((int64_t)p.chunks * (part + 1) / p.parts);
+    const int part = blockIdx.x % p.parts, c0 = (int)((int64_t)p.chunks * part / p.parts), c1 = ONE ? c0 + 1 : (int)((int64_t)p.chunks * (part + 1) / p.parts);
     const char* const base = static_cast<const char*>(p.a.logits) + row * p.a.pitch * (F32 ? 4 : 2);
-    if (TOP && tid < MAX_TOP) list[tid] = 0;
-    if (TOP && tid == 0) n_best = n_cand = 0;
-    uint64_t last = 0;   // the n_top-th key so far
-    Sums z{-INFINITY, 0.f, 0.f, 0.f};
-    for (int c = c0; c < c1; ++c) {
-        float x[PER];
-        const int first = c * CHUNK + tid * V;   // of load l: first + l * THREADS * V
+    // a chunk as it is loaded: quads of fp32, or eights of bf16; entries behind the vocabulary are -infinity
+    struct Raw { uint4 q[LOADS]; };
+    constexpr uint32_t FILL = F32 ? 0xff800000u : 0xff80ff80u;
+    auto whole = [&](int from) __attribute__((always_inline)) {
+        if constexpr (F32) return __builtin_bit_cast(uint4, *reinterpret_cast<const f32_quad*>(base + (int64_t)from * 4));
+        else return __builtin_bit_cast(uint4, *reinterpret_cast<const bf16_eight*>(base + (int64_t)from * 2));
+    };
+    auto load = [&](int c, Raw& r) __attribute__((always_inline)) {
+        const int at = c * CHUNK + tid * V;
+        if ((c + 1) * (int64_t)CHUNK <= vocab) {
+#pragma unroll
+            for (int l = 0; l < LOADS; ++l) r.q[l] = whole(at + l * (THREADS * V));
+        } else if (vocab >= V) {   // the row's last chunk: loads past its end are moved back to it, and what they have too early is shifted out
+#pragma unroll
+            for (int l = 0; l < LOADS; ++l) r.q[l] = whole(min(at + l * (THREADS * V), vocab - V));
+#pragma unroll
+            for (int l = 0; l < LOADS; ++l) r.q[l] = behind(r.q[l], max(at + l * (THREADS * V) + V - vocab, 0) * (128 / V), FILL);
+        } else {
+            auto one = [&](int i) -> uint32_t {
+                if (i >= vocab) return F32 ? 0xff800000u : 0xff80u;
+                return F32 ? reinterpret_cast<const uint32_t*>(base)[i] : reinterpret_cast<const uint16_t*>(base)[i];
+            };
+            auto word = [&](int i) { return F32 ? one(at + i) : one(at + 2 * i) | one(at + 2 * i + 1) << 16; };
+            r.q[0] = make_uint4(word(0), word(1), word(2), word(3));
+#pragma unroll
+            for (int l = 1; l < LOADS; ++l) r.q[l] = make_uint4(FILL, FILL, FILL, FILL);
+        }
+    };
+    auto values = [&](const Raw& r, float (&x)[PER]) __attribute__((always_inline)) {
 #pragma unroll
         for (int l = 0; l < LOADS; ++l) {
-            const int at = first + l * (THREADS * V);
-            if (at + V <= vocab) {
-                if constexpr (F32) {
-                    const f32_quad q = *reinterpret_cast<const f32_quad*>(base + (int64_t)at * 4);
+            const uint32_t u[4] = {r.q[l].x, r.q[l].y, r.q[l].z, r.q[l].w};
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) x[l * V + i] = q[i];
-                } else {
-                    const bf16_eight q = *reinterpret_cast<const bf16_eight*>(base + (int64_t)at * 2);
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) x[l * V + i] = bf16_to_f32(q[i]);
-                }
-            } else {
-#pragma unroll
-                for (int i = 0; i < V; ++i) {
-                    x[l * V + i] = -INFINITY;
-                    if (at + i < vocab) x[l * V + i] = F32 ? reinterpret_cast<const float*>(base)[at + i] : bf16_to_f32(reinterpret_cast<const uint16_t*>(base)[at + i]);
-                }
+            for (int i = 0; i < 4; ++i) {
+                if constexpr (F32) x[4 * l + i] = __uint_as_float(u[i]);
+                else x[8 * l + 2 * i] = bf16_lo(u[i]), x[8 * l + 2 * i + 1] = bf16_hi(u[i]);
             }
         }
+    };
+    auto id_of = [&](int c, int i) { return c * CHUNK + tid * V + i / V * (THREADS * V) + i % V; };
+
+    const Given first = p.parts == 1 ? given(p.a, row, tid) : Given{0.f, false};
+    Sums z{-INFINITY, 0.f, 0.f, 0.f};
+    int best_chunk = c0;
+    float x[PER];
+    Raw next;
+    load(c0, next);
+    for (int c = c0; c < c1; ++c) {
+        values(next, x);
+        if (!ONE && c + 1 < c1) load(c + 1, next);
         float m = -INFINITY;
 #pragma unroll
         for (int i = 0; i < PER; ++i) m = fmaxf(m, x[i]);
+        if (m > z.m) best_chunk = c;
         move_to(z, fmaxf(z.m, m));
-        {
-            const float from = z.m == -INFINITY ? 0.0f : z.m;
+        const float from = z.m == -INFINITY ? 0.0f : z.m;
+        int others = 0;
 #pragma unroll
-            for (int i = 0; i < PER; ++i) {
-                const float d = x[i] - from, e = __builtin_amdgcn_exp2f(d * LOG2E);
-                const bool top = x[i] == z.m;
-                z.c += top ? 1.0f : 0.0f;
-                z.s += top ? 0.0f : e;
-                z.e = __builtin_fmaf(fmaxf(d, -200.0f), e, z.e);
-            }
+        for (int i = 0; i < PER; ++i) {
+            const float d = x[i] - from, e = __builtin_amdgcn_exp2f(d * LOG2E);
+            const bool other = x[i] != z.m;
+            others += other;
+            z.s += other ? e : 0.0f;
+            z.e = __builtin_fmaf(fmaxf(d, -200.0f), e, z.e);
         }
-        if constexpr (TOP) {
-            // the thread's best key (elements of a thread are in the order of their ids)
-            int at = -1;
+        z.c += (float)(PER - others);
+    }
+    if constexpr (TOP) {
+        if (tid < MAX_TOP) list[tid] = 0;
+        best[tid] = 0;
+        if (tid < 8) best[THREADS + tid] = 0;
+        if (tid == 0) n_best = n_cand = n_who = 0;
+        // From which value on: the n_top-th largest of the groups of four lanes, by its upper half (0: fewer groups have a number above -infinity).
+        const uint32_t most = z.m > -INFINITY ? ordered(z.m) : 0;
+        uint32_t g = most;
+        g = max(g, (uint32_t)__shfl_xor((int)g, 1, 64));
+        g = max(g, (uint32_t)__shfl_xor((int)g, 2, 64));
+        if ((lane & 3) == 0) group[tid >> 2] = g;
+        __syncthreads();
+        const uint32_t u = group[lane];
+        uint32_t from = 0;
 #pragma unroll
-            for (int i = PER - 1; i >= 0; --i) at = x[i] == m ? i : at;
-            const int id = first + at / V * (THREADS * V) + at % V;
-            const uint64_t mine = at < 0 || id >= vocab ? 0 : key_of(m, id);
-            // from which value on: the n_top-th largest of the groups of four lanes, by its upper half
-            uint32_t g = mine > last ? (uint32_t)(mine >> 32) : 0;
-            g = max(g, (uint32_t)__shfl_xor((int)g, 1, 64));
-            g = max(g, (uint32_t)__shfl_xor((int)g, 2, 64));
-            if ((lane & 3) == 0) group[tid >> 2] = g;
+        for (int b = 31; b >= 16; --b)
+            if (__popcll(__ballot(u >= (from | 1u << b))) >= n_top) from |= 1u << b;
+        auto gather = [&](float v, int id, uint64_t low) __attribute__((always_inline)) {
+            const uint64_t key = key_of(v, id);
+            if (id >= vocab || key < low) return;
+            const int at = atomicAdd(&n_cand, 1);
+            if (at < kGathered) cand[at] = key;
+        };
+        // cand[0 .. n_cand) to its n_top largest in list; all threads, behind a barrier that closes the gathering
+        auto cut = [&]() __attribute__((always_inline)) {
+            const int total = n_cand;
+            if (tid < 8) cand[total + tid] = 0;
+            if (tid < MAX_TOP) list[tid] = 0;
             __syncthreads();
-            const uint32_t u = group[lane];
-            uint32_t from = 0;
-            for (int b = 31; b >= 16; --b)
-                if (__popcll(__ballot(u >= (from | 1u << b))) >= n_top) from |= 1u << b;
-            if (mine > last && (uint32_t)(mine >> 32) >= from) best[atomicAdd(&n_best, 1)] = mine;
+            if (tid == 0) n_cand = 0;
+            for (int i = tid; i < total; i += THREADS) {
+                const uint64_t k = cand[i];
+                const int rank = larger_keys(cand, total, k);
+                if (rank < n_top) list[rank] = k;
+            }
+            __syncthreads();
+        };
+        bool done = false;
+        if (from > 0) {   // gather all values from there on: some more than n_top, as a rule
+            const float bound = value_of(from);
+            const uint64_t low = (uint64_t)from << 32;
+            if constexpr (ONE) {
+#pragma unroll
+                for (int i = 0; i < PER; ++i)
+                    if (x[i] >= bound) gather(x[i], id_of(c0, i), low);
+            } else {
+                // the loads of the threads that have such values, dealt out to all
+                if (most >= from) who[atomicAdd(&n_who, 1)] = (uint8_t)tid;
+                __syncthreads();
+                const int n = n_who, loads = n * LOADS * (c1 - c0);
+                constexpr int AT_ONCE = 4;
+                const float one_nth = 1.0f / (float)n;
+                for (int w0 = tid; w0 < loads; w0 += AT_ONCE * THREADS) {
+                    uint4 q[AT_ONCE];
+                    int ids[AT_ONCE];
+#pragma unroll
+                    for (int b = 0; b < AT_ONCE; ++b) {
+                        const int w = min(w0 + b * THREADS, loads - 1);
+                        int l = (int)((float)w * one_nth), rest = w - l * n;   // (the product may be next to the quotient)
+                        if (rest < 0) --l, rest += n;
+                        if (rest >= n) ++l, rest -= n;
+                        ids[b] = (c0 + l / LOADS) * CHUNK + l % LOADS * (THREADS * V) + who[rest] * V;
+                        q[b] = whole(min(ids[b], vocab - V));   // (two chunks at least: more entries than V)
+                    }
+#pragma unroll
+                    for (int b = 0; b < AT_ONCE; ++b) {
+                        if (w0 + b * THREADS >= loads) break;
+                        if (ids[b] + V > vocab) q[b] = behind(q[b], (ids[b] + V - vocab) * (128 / V), FILL);
+                        const uint32_t words[4] = {q[b].x, q[b].y, q[b].z, q[b].w};
+#pragma unroll
+                        for (int i = 0; i < V; ++i) {
+                            const float v = F32 ? __uint_as_float(words[i / (V / 4)]) : i % 2 ? bf16_hi(words[i / 2]) : bf16_lo(words[i / 2]);
+                            if (v >= bound) gather(v, ids[b] + i, low);
+                        }
+                    }
+                }
+            }
+            __syncthreads();
+            done = n_cand <= kGathered;
+            if (done) cut();
+        }
+        if (!done) {
+            // Many equal values, or hardly any: the same from the n_top-th of the threads' best keys on, which at most 32 n_top keys of a chunk reach.
+            __syncthreads();
+            if (tid == 0) n_cand = 0;
+            // the thread's best key (entries of a thread are in the order of their ids); one without a number above -infinity looks for the first -infinity
+            int at = -1;
+            for (int c = best_chunk; c < c1 && at < 0; ++c) {
+                if constexpr (!ONE) {
+                    load(c, next);
+                    values(next, x);
+                }
+#pragma unroll
+                for (int i = PER - 1; i >= 0; --i) at = x[i] == z.m ? i : at;
+                best_chunk = c;
+            }
+            const int id = id_of(best_chunk, at);
+            const uint64_t mine = at < 0 || id >= vocab ? 0 : key_of(z.m, id);
+            if (mine && (uint32_t)(mine >> 32) >= from) best[atomicAdd(&n_best, 1)] = mine;
             __syncthreads();
             const int count = n_best;
-            if (count == 0) continue;   // (nothing was added: the counter stays 0; group is written again behind a barrier that follows its reads)
-            uint64_t low = max(last + 1, (uint64_t)from << 32);   // (of at most n_top threads all that can count; from > 0 takes n_top groups)
+            uint64_t low = max((uint64_t)1, (uint64_t)from << 32);   // (of at most n_top threads all that can count; from > 0 takes n_top groups)
             if (count > n_top) {
                 if (tid < count) {
                     const uint64_t k = best[tid];
-                    int rank = 0;
-                    for (int j = 0; j < count; ++j) rank += best[j] > k;
-                    if (rank == n_top - 1) floor_key = k;
+                    if (larger_keys(best, count, k) == n_top - 1) floor_key = k;
                 }
                 __syncthreads();
                 low = floor_key;
             }
-            if (mine >= low) {
+            const int at_once = ONE ? 1 : kGathered / (PER * n_top);   // chunks whose keys surely fit
+            for (int c = c0; c < c1; c += at_once) {
+                if (mine >= low) {
+                    for (int k = c; k < min(c + at_once, c1); ++k) {
+                        if constexpr (!ONE) {
+                            load(k, next);
+                            values(next, x);
+                        }
 #pragma unroll
-                for (int i = 0; i < PER; ++i) {
-                    const int e = first + i / V * (THREADS * V) + i % V;
-                    const uint64_t k = e < vocab ? key_of(x[i], e) : 0;
-                    if (k >= low) cand[atomicAdd(&n_cand, 1)] = k;
+                        for (int i = 0; i < PER; ++i) gather(x[i], id_of(k, i), low);
+                    }
                 }
+                __syncthreads();
+                if (c > c0 && tid < n_top && list[tid]) cand[atomicAdd(&n_cand, 1)] = list[tid];
+                __syncthreads();
+                cut();
+                low = max(low, list[n_top - 1]);
             }
-            if (tid < n_top && list[tid]) cand[atomicAdd(&n_cand, 1)] = list[tid];
-            __syncthreads();
-            const int total = n_cand;
-            if (tid < MAX_TOP) list[tid] = 0;
-            __syncthreads();
-            if (tid == 0) n_best = n_cand = 0;
-            largest_keys(cand, total, list, n_top);
-            __syncthreads();
-            last = list[n_top - 1];
         }
     }
     z = all_sums(z, red);
     if (p.parts == 1) {
-        write_row(p.a, row, z, list);
+        write_row(p.a, row, z, list, first);
         return;
     }
     const int64_t slot = row * p.parts + part;
@@ -222,25 +364,24 @@ __global__ void __launch_bounds__(THREADS) logprobs_kernel(LogprobsLaunch p) {
 
 // Joins the parts of a row.
 __global__ void __launch_bounds__(THREADS) logprobs_join_kernel(LogprobsLaunch p) {
-    extern __shared__ uint64_t keys[];   // [parts * n_top]
-    __shared__ Sums red[THREADS / 64];
+    extern __shared__ uint64_t keys[];   // [parts * n_top], and zeros up to a multiple of eight
+    __shared__ float4 red[THREADS / 64];
     __shared__ uint64_t list[MAX_TOP];
     const int tid = threadIdx.x, n = p.parts * p.a.n_top;
     const int64_t row = blockIdx.x;
     Sums z{-INFINITY, 0.f, 0.f, 0.f};
-    for (int i = tid; i < p.parts; i += THREADS) z = joined(z, p.part_sums[row * p.parts + i]);
-    for (int i = tid; i < n; i += THREADS) keys[i] = p.part_keys[row * n + i];
+    if (tid < p.parts) z = p.part_sums[row * p.parts + tid];
+    for (int i = tid; i < n + 8; i += THREADS) keys[i] = i < n ? p.part_keys[row * n + i] : 0;
+    const Given first = given(p.a, row, tid);
     if (tid < MAX_TOP) list[tid] = 0;
     z = all_sums(z, red);
     for (int i = tid; i < n; i += THREADS) {
         const uint64_t k = keys[i];
-        if (!k) continue;
-        int rank = 0;
-        for (int j = 0; j < n; ++j) rank += keys[j] > k;
+        const int rank = k ? larger_keys(keys, n, k) : MAX_TOP;
         if (rank < p.a.n_top) list[rank] = k;
     }
     __syncthreads();
-    write_row(p.a, row, z, list);
+    write_row(p.a, row, z, list, first);
 }
 
 constexpr int kMaxParts = 64;   // of a row: their keys lie in the joining workgroup's LDS
@@ -263,13 +404,15 @@ hipError_t launch_logprobs(const LogprobsArgs& args, hipStream_t s) {
     p.part_sums = static_cast<Sums*>(args.scratch);
     p.part_keys = reinterpret_cast<uint64_t*>(p.part_sums + (int64_t)args.rows * p.parts);
     const dim3 grid((unsigned)(args.rows * p.parts));
-    if (args.is_f32 && args.n_top) logprobs_kernel<true, true><<<grid, dim3(THREADS), 0, s>>>(p);
-    else if (args.is_f32) logprobs_kernel<true, false><<<grid, dim3(THREADS), 0, s>>>(p);
-    else if (args.n_top) logprobs_kernel<false, true><<<grid, dim3(THREADS), 0, s>>>(p);
-    else logprobs_kernel<false, false><<<grid, dim3(THREADS), 0, s>>>(p);
+    auto go = [&](auto kernel) { kernel<<<grid, dim3(THREADS), 0, s>>>(p); };
+    const bool one = p.parts == p.chunks;   // a chunk for each workgroup: it stays in registers
+    if (args.is_f32 && args.n_top) one ? go(logprobs_kernel<true, true, true>) : go(logprobs_kernel<true, true, false>);
+    else if (args.is_f32) one ? go(logprobs_kernel<true, false, true>) : go(logprobs_kernel<true, false, false>);
+    else if (args.n_top) one ? go(logprobs_kernel<false, true, true>) : go(logprobs_kernel<false, true, false>);
+    else one ? go(logprobs_kernel<false, false, true>) : go(logprobs_kernel<false, false, false>);
     if (hipError_t e = hipGetLastError()) return e;
     if (p.parts > 1) {
-        logprobs_join_kernel<<<dim3((unsigned)args.rows), dim3(THREADS), (size_t)p.parts * args.n_top * 8, s>>>(p);
+        logprobs_join_kernel<<<dim3((unsigned)args.rows), dim3(THREADS), ((size_t)p.parts * args.n_top + 8) * 8, s>>>(p);
         return hipGetLastError();
     }
     return hipSuccess;

@@ -131,6 +131,7 @@ def test_rows_that_are_hard(rs, v, dtype):
     x[14, :32] = 60.0                                                # all alternatives in one thread's reach, and ties behind them
     x[15, :] = torch.where(torch.arange(v, device="cuda") % 1024 < 4, 9.0, -1.0)
     ids = torch.arange(16 * 4, device="cuda", dtype=torch.int32).view(16, 4) % v
+    x[8, v // 2:] = -inf                                             # no number above -infinity, NaN ahead of them
     _check(rs, x.to(dtype), ids, min(32, 20), f"hard rows of {v}")
 
 
