@@ -4,13 +4,13 @@
 // Z = c + s and log Z = log1p((c - 1) + s), so that a nearly sure row keeps the digits of a log probability next to 0; both terms of H are
 // positive, so nothing cancels in it.
 //
-// A workgroup of 256 threads holds 8192 values of a row at a time, 32 a thread, while the next ones are on their way.  Nothing in that pass waits for
+// A workgroup holds 32 values a thread of a row at a time (8192 of 256 threads) while the next ones are on their way.  Nothing in that pass waits for
 // another thread; a thread remembers its largest value and the chunk it came in.
 //
 // Alternatives are 64-bit keys, the value's bits in an order of whole numbers above the id's complement: larger value first, the lower id among
-// equals, all keys different.  Behind the pass the largest values of the groups of four lanes give a bound that n_top values reach at least; the
+// equals, all keys different.  Behind the pass the largest values of 64 groups of lanes give a bound that n_top values reach at least; the
 // loads of the threads whose largest value reaches it are dealt out to all threads once more (from the caches), and what reaches the bound is
-// gathered and ranked.  Where ties let too much reach it, the bound is the n_top-th of the 256 threads' best keys.
+// gathered and ranked.  Where ties let too much reach it, the bound is the n_top-th of the threads' best keys.
 //
 // Few rows are cut into parts of whole chunks for several workgroups, whose results a second launch joins in their order.
 #include <algorithm>
@@ -22,7 +22,8 @@ namespace relserve {
 
 namespace {
 
-constexpr int THREADS = 256, PER = 32, CHUNK = THREADS * PER, MAX_TOP = 32;
+constexpr int PER = 32, MAX_TOP = 32;      // values a thread holds at a time; alternatives
+constexpr int FEW = 256, MANY = 1024;      // threads of a workgroup
 constexpr float LOG2E = 1.4426950408889634f;
 
 struct Sums {
@@ -71,6 +72,7 @@ __device__ __forceinline__ Given given(const LogprobsArgs& a, int64_t row, int j
 }
 
 // What is left to do when a row's sums and keys are known.
+template <int THREADS>
 __device__ __forceinline__ void write_row(const LogprobsArgs& a, int64_t row, const Sums& z, const uint64_t* keys, Given first) {
     const float lz = log_z(z);
     const int tid = threadIdx.x;
@@ -87,6 +89,7 @@ __device__ __forceinline__ void write_row(const LogprobsArgs& a, int64_t row, co
 }
 
 // The sums of all threads, in every thread: moved to the largest value of all, then added.
+template <int THREADS>
 __device__ __forceinline__ Sums all_sums(Sums z, float4* red) {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     float m = z.m;
@@ -141,15 +144,16 @@ __device__ __forceinline__ uint4 behind(const uint4& q, int bits, uint32_t fill)
 
 constexpr int kGathered = 2048;   // keys that a workgroup gathers at most: two chunks' of 32 alternatives
 
-template <bool F32, bool TOP, bool ONE>
+template <int THREADS, bool F32, bool TOP, bool ONE>
 __global__ void __launch_bounds__(THREADS) logprobs_kernel(LogprobsLaunch p) {
+    constexpr int CHUNK = THREADS * PER, GROUP = THREADS / 64;   // values of a chunk; lanes of a group: 64 groups
     constexpr int V = F32 ? 4 : 8, LOADS = PER / V;   // values of a load
     typedef float f32_quad __attribute__((ext_vector_type(4), aligned(4)));
     typedef uint16_t bf16_eight __attribute__((ext_vector_type(8), aligned(2)));
     __shared__ float4 red[THREADS / 64];
     __shared__ uint64_t list[TOP ? MAX_TOP : 1], best[TOP ? THREADS + 8 : 1], cand[TOP ? kGathered + MAX_TOP + 8 : 1], floor_key;
     __shared__ uint32_t group[TOP ? 64 : 1];
-    __shared__ uint8_t who[TOP && !ONE ? THREADS : 1];
+    __shared__ uint16_t who[TOP && !ONE ? THREADS : 1];
     __shared__ int n_best, n_cand, n_who;
     const int tid = threadIdx.x, lane = tid & 63, vocab = p.a.vocab, n_top = p.a.n_top;
     const int64_t row = blockIdx.x / p.parts;
@@ -227,12 +231,12 @@ __global__ void __launch_bounds__(THREADS) logprobs_kernel(LogprobsLaunch p) {
         best[tid] = 0;
         if (tid < 8) best[THREADS + tid] = 0;
         if (tid == 0) n_best = n_cand = n_who = 0;
-        // From which value on: the n_top-th largest of the groups of four lanes, by its upper half (0: fewer groups have a number above -infinity).
+        // From which value on: the n_top-th largest of the 64 groups of lanes, by its upper half (0: fewer groups have a number above -infinity).
         const uint32_t most = z.m > -INFINITY ? ordered(z.m) : 0;
         uint32_t g = most;
-        g = max(g, (uint32_t)__shfl_xor((int)g, 1, 64));
-        g = max(g, (uint32_t)__shfl_xor((int)g, 2, 64));
-        if ((lane & 3) == 0) group[tid >> 2] = g;
+#pragma unroll
+        for (int o = 1; o < GROUP; o *= 2) g = max(g, (uint32_t)__shfl_xor((int)g, o, 64));
+        if (tid % GROUP == 0) group[tid / GROUP] = g;
         __syncthreads();
         const uint32_t u = group[lane];
         uint32_t from = 0;
@@ -269,7 +273,7 @@ __global__ void __launch_bounds__(THREADS) logprobs_kernel(LogprobsLaunch p) {
                     if (x[i] >= bound) gather(x[i], id_of(c0, i), low);
             } else {
                 // the loads of the threads that have such values, dealt out to all
-                if (most >= from) who[atomicAdd(&n_who, 1)] = (uint8_t)tid;
+                if (most >= from) who[atomicAdd(&n_who, 1)] = (uint16_t)tid;
                 __syncthreads();
                 const int n = n_who, loads = n * LOADS * (c1 - c0);
                 constexpr int AT_ONCE = 4;
@@ -352,9 +356,9 @@ __global__ void __launch_bounds__(THREADS) logprobs_kernel(LogprobsLaunch p) {
             }
         }
     }
-    z = all_sums(z, red);
+    z = all_sums<THREADS>(z, red);
     if (p.parts == 1) {
-        write_row(p.a, row, z, list, first);
+        write_row<THREADS>(p.a, row, z, list, first);
         return;
     }
     const int64_t slot = row * p.parts + part;
@@ -363,32 +367,45 @@ __global__ void __launch_bounds__(THREADS) logprobs_kernel(LogprobsLaunch p) {
 }
 
 // Joins the parts of a row.
-__global__ void __launch_bounds__(THREADS) logprobs_join_kernel(LogprobsLaunch p) {
+__global__ void __launch_bounds__(FEW) logprobs_join_kernel(LogprobsLaunch p) {
     extern __shared__ uint64_t keys[];   // [parts * n_top], and zeros up to a multiple of eight
-    __shared__ float4 red[THREADS / 64];
+    __shared__ float4 red[FEW / 64];
     __shared__ uint64_t list[MAX_TOP];
     const int tid = threadIdx.x, n = p.parts * p.a.n_top;
     const int64_t row = blockIdx.x;
     Sums z{-INFINITY, 0.f, 0.f, 0.f};
     if (tid < p.parts) z = p.part_sums[row * p.parts + tid];
-    for (int i = tid; i < n + 8; i += THREADS) keys[i] = i < n ? p.part_keys[row * n + i] : 0;
+    for (int i = tid; i < n + 8; i += FEW) keys[i] = i < n ? p.part_keys[row * n + i] : 0;
     const Given first = given(p.a, row, tid);
     if (tid < MAX_TOP) list[tid] = 0;
-    z = all_sums(z, red);
-    for (int i = tid; i < n; i += THREADS) {
+    z = all_sums<FEW>(z, red);
+    for (int i = tid; i < n; i += FEW) {
         const uint64_t k = keys[i];
         const int rank = k ? larger_keys(keys, n, k) : MAX_TOP;
         if (rank < p.a.n_top) list[rank] = k;
     }
     __syncthreads();
-    write_row(p.a, row, z, list, first);
+    write_row<FEW>(p.a, row, z, list, first);
 }
 
 constexpr int kMaxParts = 64;   // of a row: their keys lie in the joining workgroup's LDS
 
+// About as many rows as CUs, each of which a large workgroup holds at once: no second launch (200 x 32000, in parts and in one: fp32 13.7 -> 11.3 us, bf16
+// with 20 alternatives 16.3 -> 13.3).  Fewer rows are faster in parts, a CU's vector units being what a row waits for (24 x 32000 with five
+// alternatives 10.4 in parts, 11.9 in one), and so are shorter ones (256 x 16000 13.4, 13.8).
+bool large_workgroups(int64_t rows, int64_t vocab) { return rows >= 64 && rows <= 256 && vocab > 2 * FEW * PER && vocab <= MANY * PER; }
+
 int32_t parts_of(int64_t rows, int64_t vocab) {
-    const int64_t chunks = (vocab + CHUNK - 1) / CHUNK;
+    if (large_workgroups(rows, vocab)) return 1;
+    const int64_t chunks = (vocab + FEW * PER - 1) / (FEW * PER);
     return (int32_t)std::min<int64_t>({chunks, kMaxParts, std::max<int64_t>(1, 512 / std::max<int64_t>(1, rows))});
+}
+
+template <int THREADS, bool ONE>
+void launch_rows(const LogprobsLaunch& p, hipStream_t s) {
+    auto go = [&](auto kernel) { kernel<<<dim3((unsigned)(p.a.rows * p.parts)), dim3(THREADS), 0, s>>>(p); };
+    if (p.a.is_f32) p.a.n_top ? go(logprobs_kernel<THREADS, true, true, ONE>) : go(logprobs_kernel<THREADS, true, false, ONE>);
+    else p.a.n_top ? go(logprobs_kernel<THREADS, false, true, ONE>) : go(logprobs_kernel<THREADS, false, false, ONE>);
 }
 
 }  // namespace
@@ -400,19 +417,17 @@ int64_t logprobs_scratch_bytes(int64_t rows, int64_t vocab, int64_t n_top) {
 
 hipError_t launch_logprobs(const LogprobsArgs& args, hipStream_t s) {
     if (args.rows == 0) return hipSuccess;
-    LogprobsLaunch p{args, args.scratch ? parts_of(args.rows, args.vocab) : 1, (int32_t)(((int64_t)args.vocab + CHUNK - 1) / CHUNK), nullptr, nullptr};
+    const bool large = large_workgroups(args.rows, args.vocab);
+    const int32_t chunk = (large ? MANY : FEW) * PER;
+    LogprobsLaunch p{args, args.scratch ? parts_of(args.rows, args.vocab) : 1, (int32_t)(((int64_t)args.vocab + chunk - 1) / chunk), nullptr, nullptr};
     p.part_sums = static_cast<Sums*>(args.scratch);
     p.part_keys = reinterpret_cast<uint64_t*>(p.part_sums + (int64_t)args.rows * p.parts);
-    const dim3 grid((unsigned)(args.rows * p.parts));
-    auto go = [&](auto kernel) { kernel<<<grid, dim3(THREADS), 0, s>>>(p); };
-    const bool one = p.parts == p.chunks;   // a chunk for each workgroup: it stays in registers
-    if (args.is_f32 && args.n_top) one ? go(logprobs_kernel<true, true, true>) : go(logprobs_kernel<true, true, false>);
-    else if (args.is_f32) one ? go(logprobs_kernel<true, false, true>) : go(logprobs_kernel<true, false, false>);
-    else if (args.n_top) one ? go(logprobs_kernel<false, true, true>) : go(logprobs_kernel<false, true, false>);
-    else one ? go(logprobs_kernel<false, false, true>) : go(logprobs_kernel<false, false, false>);
+    if (large) launch_rows<MANY, true>(p, s);
+    else if (p.parts == p.chunks) launch_rows<FEW, true>(p, s);   // a chunk for each workgroup: it stays in registers
+    else launch_rows<FEW, false>(p, s);
     if (hipError_t e = hipGetLastError()) return e;
     if (p.parts > 1) {
-        logprobs_join_kernel<<<dim3((unsigned)args.rows), dim3(THREADS), ((size_t)p.parts * args.n_top + 8) * 8, s>>>(p);
+        logprobs_join_kernel<<<dim3((unsigned)args.rows), dim3(FEW), ((size_t)p.parts * args.n_top + 8) * 8, s>>>(p);
         return hipGetLastError();
     }
     return hipSuccess;

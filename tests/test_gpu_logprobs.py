@@ -97,7 +97,7 @@ def _logits(seed, t, v, dtype):
 
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=["f32", "bf16"])
 @pytest.mark.parametrize("t,v,top", [(1, 1, 1), (2, 5, 32), (3, 100, 0), (7, 1000, 5), (1, 8192, 20), (2, 8193, 32), (24, 32000, 5), (5, 50257, 20),
-                                     (1, 152065, 32), (300, 4097, 1), (600, 16387, 7), (1, 600001, 32)])
+                                     (1, 152065, 32), (300, 4097, 1), (600, 16387, 7), (1, 600001, 32), (70, 31999, 9)])
 def test_sizes(rs, t, v, top, dtype):
     x, ids = _logits(t * 3 + v, t, v, dtype)
     ids[-1, -1] = v
