@@ -716,7 +716,18 @@ hipError_t run(const Args& p, hipStream_t s) { return run_plan<EPI>(p, plan_for(
 
 }  // namespace
 
-int64_t gemm_f8b_scratch_floats(int64_t T, int64_t N) { return 2 * T * N > kSlabFloats ? 64 : std::max<int64_t>(64, std::min(16 * T * N, kSlabFloats)); }
+// (grows with either size, so that the largest call's serves all)
+int64_t gemm_f8b_scratch_floats(int64_t T, int64_t N) { return std::max<int64_t>(64, std::min(16 * T * N, kSlabFloats)); }
+
+GemmPlanF8b gemm_plan_f8b(int32_t T, int32_t N, int32_t K, int32_t epilogue, bool scratch) {
+    float some_scratch;
+    Args p{};
+    p.T = T, p.N = N, p.K = K, p.n_half = N / 2;
+    p.slabs = scratch ? &some_scratch : nullptr;
+    const Plan plan = plan_for(p, epilogue);
+    const int per_range = (K / KB + plan.splits - 1) / plan.splits;
+    return {plan.tile, (K / KB + per_range - 1) / per_range};
+}
 
 hipError_t launch_linear_f8b(const void* a, const float* a_scale, const void* w, const float* w_scale, int32_t T, int32_t N, int32_t K,
                              int32_t epilogue, const void* residual, void* out, hipStream_t s, float* scratch, bool w_packed) {

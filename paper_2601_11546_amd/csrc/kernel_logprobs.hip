@@ -388,7 +388,8 @@ __global__ void __launch_bounds__(FEW) logprobs_join_kernel(LogprobsLaunch p) {
     write_row<FEW>(p.a, row, z, list, first);
 }
 
-constexpr int kMaxParts = 64;   // of a row: their keys lie in the joining workgroup's LDS
+constexpr int kMaxParts = 64;     // of a row: their keys lie in the joining workgroup's LDS
+constexpr int kMostParts = 512;   // of all rows that are cut: two workgroups for each CU
 
 // About as many rows as CUs, each of which a large workgroup holds at once: no second launch (200 x 32000, in parts and in one: fp32 13.7 -> 11.3 us, bf16
 // with 20 alternatives 16.3 -> 13.3).  Fewer rows are faster in parts, a CU's vector units being what a row waits for (24 x 32000 with five
@@ -398,7 +399,7 @@ bool large_workgroups(int64_t rows, int64_t vocab) { return rows >= 64 && rows <
 int32_t parts_of(int64_t rows, int64_t vocab) {
     if (large_workgroups(rows, vocab)) return 1;
     const int64_t chunks = (vocab + FEW * PER - 1) / (FEW * PER);
-    return (int32_t)std::min<int64_t>({chunks, kMaxParts, std::max<int64_t>(1, 512 / std::max<int64_t>(1, rows))});
+    return (int32_t)std::min<int64_t>({chunks, kMaxParts, std::max<int64_t>(1, kMostParts / std::max<int64_t>(1, rows))});
 }
 
 template <int THREADS, bool ONE>
@@ -410,10 +411,8 @@ void launch_rows(const LogprobsLaunch& p, hipStream_t s) {
 
 }  // namespace
 
-int64_t logprobs_scratch_bytes(int64_t rows, int64_t vocab, int64_t n_top) {
-    const int64_t parts = parts_of(rows, vocab);
-    return parts > 1 ? rows * parts * ((int64_t)sizeof(Sums) + 8 * n_top) : 0;
-}
+// (grows with the rows, so that the largest call's serves all: of whatever rows there are, at most kMostParts parts)
+int64_t logprobs_scratch_bytes(int64_t rows, int64_t n_top) { return std::min<int64_t>(rows * kMaxParts, kMostParts) * ((int64_t)sizeof(Sums) + 8 * n_top); }
 
 hipError_t launch_logprobs(const LogprobsArgs& args, hipStream_t s) {
     if (args.rows == 0) return hipSuccess;

@@ -69,7 +69,7 @@ int32_t relserve_linear_f8b(const void* a, const float* a_scale, const void* w, 
 int32_t relserve_logprobs_workspace_bytes(int32_t n_rows, int32_t vocab, int32_t n_top, size_t* out) {
     if (!out) return RELSERVE_ERR_NULL_POINTER;
     if (n_rows < 0 || vocab <= 0 || n_top < 0 || n_top > kMaxTop) return RELSERVE_ERR_BAD_ARGUMENT;
-    *out = (size_t)logprobs_scratch_bytes(n_rows, vocab, n_top);
+    *out = (size_t)logprobs_scratch_bytes(n_rows, n_top);
     return RELSERVE_OK;
 }
 
@@ -84,7 +84,7 @@ int32_t relserve_logprobs(const void* logits, int32_t logits_are_f32, int32_t n_
     if (!aligned(logits, logits_are_f32 ? 4 : 2) || !aligned(ids, 4) || !aligned(logprobs, 4) || !aligned(entropy, 4) || !aligned(top_ids, 4) ||
         !aligned(top_logprobs, 4))
         return RELSERVE_ERR_BAD_ARGUMENT;
-    if (workspace && (!aligned(workspace, kAlign) || workspace_bytes < (size_t)logprobs_scratch_bytes(n_rows, vocab, n_top))) return RELSERVE_ERR_WORKSPACE;
+    if (workspace && (!aligned(workspace, kAlign) || workspace_bytes < (size_t)logprobs_scratch_bytes(n_rows, n_top))) return RELSERVE_ERR_WORKSPACE;
     const LogprobsArgs args{logits, logits_are_f32 != 0, n_rows, vocab, pitch, ids, n_ids, logprobs, entropy, n_top, top_ids, top_logprobs, workspace};
     return launch_logprobs(args, static_cast<hipStream_t>(stream)) == hipSuccess ? RELSERVE_OK : RELSERVE_ERR_HIP;
 }

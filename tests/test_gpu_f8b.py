@@ -7,6 +7,8 @@ import numpy as np
 import pytest
 import torch
 
+from tests import f8b_paths
+
 pytestmark = pytest.mark.gpu
 
 U, B = 2.0 ** -24, 2.0 ** -8
@@ -241,6 +243,18 @@ def test_linear(rs, t, n, k, epilogue):
         _check_linear(got, y, size, p[4], epilogue, k, f"{t} x {n} x {k}")
     assert torch.equal(results[0], _run_linear(rs, p, epilogue, packed, True, n))            # the same bits every time
     assert torch.equal(results[0], _run_linear(rs, p, epilogue, not packed, True, n))        # and from either layout
+
+
+@pytest.mark.parametrize("size", f8b_paths.SIZES, ids=str)
+def test_paths(rs, size):
+    """Every tile, whole and in k ranges, in either layout of the weights."""
+    t, n, k, epilogue = size
+    print(f"[case] path {f8b_paths.SIZES[size]}: {size}", flush=True)
+    p = _problem(_gen(t + n + k), t, n, k, epilogue, False)
+    y, bound = _reference(*p, epilogue)
+    got = _run_linear(rs, p, epilogue, False, True, n)
+    _check_linear(got, y, bound, p[4], epilogue, k, str(size))
+    assert torch.equal(got, _run_linear(rs, p, epilogue, True, True, n))
 
 
 def test_no_residual_is_a_residual_of_zeros(rs):

@@ -106,8 +106,8 @@ def test_sizes(rs, t, v, top, dtype):
 
 
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=["f32", "bf16"])
-@pytest.mark.parametrize("v", [60, 9001, 40000])
-def test_rows_that_are_hard(rs, v, dtype):
+@pytest.mark.parametrize("v,times", [(60, 1), (9001, 1), (40000, 1), (20000, 5)])
+def test_rows_that_are_hard(rs, v, times, dtype):
     inf, nan = float("inf"), float("nan")
     x, _ = _logits(v, 16, v, torch.float32)
     x[0] = 0.0                                                       # all alike
@@ -132,7 +132,7 @@ def test_rows_that_are_hard(rs, v, dtype):
     x[15, :] = torch.where(torch.arange(v, device="cuda") % 1024 < 4, 9.0, -1.0)
     ids = torch.arange(16 * 4, device="cuda", dtype=torch.int32).view(16, 4) % v
     x[8, v // 2:] = -inf                                             # no number above -infinity, NaN ahead of them
-    _check(rs, x.to(dtype), ids, min(32, 20), f"hard rows of {v}")
+    _check(rs, x.to(dtype).repeat(times, 1), ids.repeat(times, 1), 20, f"hard rows of {v}")
 
 
 def test_columns_behind_the_vocabulary_are_not_read(rs):
