@@ -418,20 +418,21 @@ def pack_layer_weights_w8a8(weights: dict) -> dict:
     return out
 
 
-def _dense(where: str, *tensors) -> None:
-    """The int8 entry points take whole row-major matrices on the current device, of the types and shapes named: (name, tensor, dtype, shape)."""
-    device = None
+def _dense(where: str, *tensors, device=None) -> None:
+    """The int8 and the block-scaled entry points take whole row-major matrices on the current device, of the types and shapes named: (name, tensor,
+    dtype, shape).  device: where another operand lies."""
     for name, t, dtype, shape in tensors:
         if t is None:
             continue
         if t.dtype is not dtype or t.shape != shape or not t.is_contiguous():
             raise ValueError(f"{where}: {name} must be a contiguous {dtype} tensor of shape {tuple(shape)}, "
                              f"not {t.dtype} {tuple(t.shape)} with strides {t.stride()}")
-        if device is None:
-            device = t.get_device()
-        elif t.get_device() != device:
-            raise ValueError(f"{where}: {name} lies on {t.device}, other tensors elsewhere")
-    if device < 0 or device != torch.cuda.current_device():
+        at = t.get_device()
+        if at != device:
+            if device is not None:
+                raise ValueError(f"{where}: {name} lies on {t.device}, other tensors elsewhere")
+            device = at
+    if device < 0 or device != torch._C._cuda_getDevice():   # (a tensor on a device: the runtime is up)
         raise ValueError(f"{where}: the tensors do not lie on the current device")
 
 
@@ -613,18 +614,19 @@ def relserve_logprobs(logits, ids=None, logprobs=None, entropy=None, top_ids=Non
     fp32; entropy [rows] fp32; top_ids [rows, k] int32 and top_logprobs [rows, k] fp32.  workspace: uint8 tensor of relserve_logprobs_workspace_bytes
     bytes or more, or None."""
     rows, vocab = logits.shape
+    pitch, step = logits.stride()
     f32 = logits.dtype is torch.float32
-    if (logits.dtype is not torch.bfloat16 and not f32) or (vocab > 1 and logits.stride(1) != 1) or (rows > 1 and logits.stride(0) < vocab):
+    if not (f32 or logits.dtype is torch.bfloat16) or (step != 1 and vocab > 1) or (pitch < vocab and rows > 1):
         raise ValueError(f"relserve_logprobs: logits must be rows of fp32 or bf16 entries one behind the other, not {logits.dtype} with strides "
                          f"{logits.stride()}")
     if (ids is None) != (logprobs is None) or (top_ids is None) != (top_logprobs is None):
         raise ValueError("relserve_logprobs: ids and logprobs, top_ids and top_logprobs are given together")
     n_ids, n_top = 0 if ids is None else ids.shape[1], 0 if top_ids is None else top_ids.shape[1]
-    _dense("relserve_logprobs", ("logits", logits[:1, :1].reshape(-1) if rows else logits.reshape(-1), logits.dtype, (min(rows, 1),)),
-           ("ids", ids, torch.int32, (rows, n_ids)), ("logprobs", logprobs, torch.float32, (rows, n_ids)), ("entropy", entropy, torch.float32, (rows,)),
-           ("top_ids", top_ids, torch.int32, (rows, n_top)), ("top_logprobs", top_logprobs, torch.float32, (rows, n_top)),
-           ("workspace", workspace, torch.uint8, workspace.shape if workspace is not None else ()))
-    _check(_lib.relserve_logprobs(logits.data_ptr(), f32, rows, vocab, logits.stride(0) if rows > 1 else vocab, _address(ids), n_ids,
+    _dense("relserve_logprobs", ("ids", ids, torch.int32, (rows, n_ids)), ("logprobs", logprobs, torch.float32, (rows, n_ids)),
+           ("entropy", entropy, torch.float32, (rows,)), ("top_ids", top_ids, torch.int32, (rows, n_top)),
+           ("top_logprobs", top_logprobs, torch.float32, (rows, n_top)),
+           ("workspace", workspace, torch.uint8, workspace.shape if workspace is not None else ()), device=logits.get_device())
+    _check(_lib.relserve_logprobs(logits.data_ptr(), f32, rows, vocab, pitch if rows > 1 else vocab, _address(ids), n_ids,
                                   _address(logprobs), _address(entropy), n_top, _address(top_ids), _address(top_logprobs), _address(workspace),
                                   0 if workspace is None else workspace.numel(), _stream_address(logits, stream)), "relserve_logprobs")
 

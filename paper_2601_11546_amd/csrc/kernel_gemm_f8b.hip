@@ -678,10 +678,17 @@ Plan plan_for(const Args& p, int epi) {
     return best;
 }
 
+// Up to 16 tokens weights of 32 MB and more are read with the non-temporal hint: two layers with such a matrix are more than the last-level cache holds, so
+// that the next step finds them in memory.  us without -> with, from memory (from the cache): T = 1, 15360 x 5120 15.2 -> 14.2 (13.2, 13.2), SwiGLU 27648 x
+// 5120 26.3 -> 24.1, T = 16, 12288 x 4096 12.7 -> 12.1 (9.8 -> 10.7).  At 24 tokens it loses more from the cache than it gains (15360 x 5120 18.1 -> 17.7, 14.0 -> 16.2).
+constexpr int64_t kFarWeights = (int64_t)32 << 20;
+
 template <int EPI, bool WIDE>
 hipError_t run_tile(const Args& p, Plan plan, hipStream_t s) {
     switch (plan.tile) {
-        case ROWS_16: return launch_rows<EPI, 2, 1, 4, 3, WIDE, false>(p, plan.splits, s);
+        case ROWS_16:
+            return (int64_t)p.N * p.K >= kFarWeights ? launch_rows<EPI, 2, 1, 4, 3, WIDE, true>(p, plan.splits, s)
+                                                     : launch_rows<EPI, 2, 1, 4, 3, WIDE, false>(p, plan.splits, s);
         case ROWS_16_NARROW:
             if constexpr (EPI != EPI_SWIGLU) return launch_rows<EPI, 1, 1, 4, 4, WIDE, false>(p, plan.splits, s);
             else return hipErrorInvalidValue;
