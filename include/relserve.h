@@ -306,8 +306,8 @@ int32_t relserve_greedy_sample(const void* logits, int32_t n_rows, int32_t vocab
  * logits: device, fp32 (logits_are_f32 != 0) or bf16, row r begins at element r * pitch (pitch >= vocab: columns behind the vocabulary are not read).
  * ids [n_rows, n_ids], logprobs [n_rows, n_ids] fp32, entropy [n_rows] fp32 (or NULL), top_ids [n_rows, n_top], top_logprobs [n_rows, n_top] fp32; n_ids
  * and n_top may be 0 (with NULL arrays), n_top at most 32.  n_rows at most 2^22, vocab 2^24 (RELSERVE_ERR_TOO_LARGE).  workspace: scratch as in
- * relserve_layer_step, of at least relserve_logprobs_workspace_bytes bytes (140 KB at most, growing with n_rows and n_top): a few rows are cut into parts for several workgroups.  With NULL they are not
- * cut: last bits may differ, and few rows take longer. */
+ * relserve_layer_step, of at least relserve_logprobs_workspace_bytes bytes (140 KB at most, growing with n_rows and n_top): a few rows are
+ * cut into parts for several workgroups.  With NULL they are not cut: last bits may differ, and few rows take longer. */
 int32_t relserve_logprobs_workspace_bytes(int32_t n_rows, int32_t vocab, int32_t n_top, size_t* out);
 int32_t relserve_logprobs(const void* logits, int32_t logits_are_f32, int32_t n_rows, int32_t vocab, int64_t pitch, const int32_t* ids,
                           int32_t n_ids, float* logprobs, float* entropy, int32_t n_top, int32_t* top_ids, float* top_logprobs,
@@ -413,14 +413,16 @@ int32_t relserve_layer_step_i8(const relserve_layer* layer, const relserve_batch
  * relserve_add_rmsnorm_f8b: relserve_add_rmsnorm_i8 with these codes: s = x + delta, rounded to x's type, kept in sum if given (which may be x, and overlaps
  * nothing else); codes and scales [hidden / 128, n_rows] of s * w / sqrt(mean(s^2) + eps).
  *
- * relserve_linear_f8b: out[t, n] = sum over blocks b of k of (sum over k in b of a[t, k] * w[n, k]) * (a_scale[b, t] * w_scale[n / 128, b]) on codes: a block's
- * products exact, its sum in fp32, added with one fused multiply-add; epilogues, residuals and outputs as relserve_linear (0 and 3 read no residual).
- * K a multiple of 128, N of 4 (of 16 for SwiGLU), T K and N K below 2^31 (RELSERVE_ERR_TOO_LARGE).  With SwiGLU the gate's and the up's rows are blocked each from their own first one: w_scale
- * [2 ceil(N / 256), K / 128].  packed != 0: w is relserve_pack_weight applied to the matrix seen as [N, K / 2] two-byte units.  workspace: scratch
- * as in relserve_layer_step, of at least relserve_linear_f8b_workspace_bytes(T, N) bytes (64 MB at most, growing with either): holds partial sums where
- * k is cut into ranges for several workgroups.  With NULL k is never cut: last bits may differ, and few tokens or outputs on long k take longer.
- * The matrix instruction on 8-bit codes drops what lies some 14 bits below the largest of a few neighbouring products: bf16 outputs are off by up to 2e-5
- * of a row's norm beside their own rounding.  fp32 outputs (epilogue 1) are right to fp32: there codes are multiplied as bf16 values. */
+ * relserve_linear_f8b: out[t, n] = sum over blocks b of k of (sum over k in b of a[t, k] * w[n, k]) * (a_scale[b, t] * w_scale[n / 128, b]) on codes, a
+ * block's sum added with one fused multiply-add in fp32; epilogues, residuals and outputs as relserve_linear (0 and 3 read no residual).
+ * For fp32 outputs (epilogue 1) a block's products are exact and its sum is one of fp32: codes are multiplied as bf16 values.  bf16 outputs use the
+ * matrix instruction on 8-bit codes, which drops what lies some 14 bits below the largest of a few neighbouring products: they are off by up to 2e-5 of a
+ * row's norm beside their own rounding.
+ * K a multiple of 128, N of 4 (of 16 for SwiGLU), T K and N K below 2^31 (RELSERVE_ERR_TOO_LARGE).  With SwiGLU the gate's and the up's rows are blocked
+ * each from their own first one: w_scale [2 ceil(N / 256), K / 128].  packed != 0: w is relserve_pack_weight applied to the matrix seen as [N, K / 2]
+ * two-byte units.  workspace: scratch as in relserve_layer_step, of at least relserve_linear_f8b_workspace_bytes(T, N) bytes (64 MB at most, growing
+ * with either): holds partial sums where k is cut into ranges for several workgroups.  With NULL k is never cut: last bits may differ, and few tokens
+ * or outputs on long k take longer. */
 int32_t relserve_quantise_f8b(const void* in, int32_t n_rows, int32_t n, int32_t block_rows, void* codes, float* scales, void* stream);
 int32_t relserve_add_rmsnorm_f8b(const void* x, int32_t x_is_f32, const void* delta, const void* w, float eps, int32_t n_rows,
                                  int32_t hidden, void* sum, void* codes, float* scales, void* stream);

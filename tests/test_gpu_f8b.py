@@ -217,8 +217,11 @@ def _run_linear(rs, p, epilogue, packed, scratch, n, stream=None):
     t = a.shape[0]
     full, out = _with_guard(t, n // 2 if epilogue == 3 else n, dtype=torch.float32 if epilogue == 1 else torch.bfloat16, fill=7.0)
     ws = torch.full((max(256, rs.relserve_linear_f8b_workspace_bytes(t, n)),), 255, dtype=torch.uint8, device="cuda") if scratch else None
-    rs.relserve_linear_f8b(a, a_scale, rs.pack_codes(w) if packed else w, w_scale, epilogue, residual, out, n=n if packed else 0, workspace=ws,
-                           stream=stream)
+    if packed:
+        w = rs.pack_codes(w)
+    if stream is not None:
+        stream.wait_stream(torch.cuda.current_stream())   # the fills above too
+    rs.relserve_linear_f8b(a, a_scale, w, w_scale, epilogue, residual, out, n=n if packed else 0, workspace=ws, stream=stream)
     torch.cuda.synchronize()
     assert bool((full[t:] == 7.0).all())
     return out
@@ -353,6 +356,4 @@ def test_replays_of_a_captured_chain(rs):
 def test_another_stream(rs):
     p = _problem(_gen(3), 40, 768, 2048, 1, False)
     want = _run_linear(rs, p, 1, False, True, 768)
-    side = torch.cuda.Stream()
-    side.wait_stream(torch.cuda.current_stream())
-    assert torch.equal(_run_linear(rs, p, 1, False, True, 768, stream=side), want)
+    assert torch.equal(_run_linear(rs, p, 1, False, True, 768, stream=torch.cuda.Stream()), want)

@@ -26,6 +26,8 @@ def _call(rs, logits, ids=None, n_top=0, scratch=True, stream=None):
             "id": torch.full((t + GUARD, n_top), 77, dtype=torch.int32, device="cuda"), "tlp": torch.full((t + GUARD, n_top), 5.0, device="cuda")}
     need = rs.relserve_logprobs_workspace_bytes(t, v, n_top)
     ws = torch.full((max(256, need),), 255, dtype=torch.uint8, device="cuda") if scratch else None
+    if stream is not None:
+        stream.wait_stream(torch.cuda.current_stream())   # the fills above too
     rs.relserve_logprobs(logits, ids, None if ids is None else full["lp"][:t], full["h"][:t], full["id"][:t] if n_top else None,
                          full["tlp"][:t] if n_top else None, workspace=ws, stream=stream)
     torch.cuda.synchronize()
@@ -160,9 +162,7 @@ def test_nothing_asked_but_the_entropy(rs):
 def test_another_stream_and_the_same_bits(rs):
     x, ids = _logits(9, 3, 70000, torch.float32)
     want = _call(rs, x, ids, 10)
-    side = torch.cuda.Stream()
-    side.wait_stream(torch.cuda.current_stream())
-    for got in (_call(rs, x, ids, 10), _call(rs, x, ids, 10, stream=side)):
+    for got in (_call(rs, x, ids, 10), _call(rs, x, ids, 10, stream=torch.cuda.Stream())):
         assert all(torch.equal(a, b) for a, b in zip(got, want))
 
 
