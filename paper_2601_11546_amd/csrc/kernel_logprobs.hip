@@ -1,19 +1,24 @@
 // Log probabilities of rows of logits: of given tokens, the row's entropy, and its top alternatives.
 //   m = max x,  Z = sum e^(x - m),  log p(i) = (x[i] - m) - log Z,  H = log Z - (sum (x - m) e^(x - m)) / Z
-// One pass: a thread keeps the running (m, c, s, E): how often it has met its largest value, the sum over the others, and sum (x - m) e^(x - m).
-// Z = c + s and log Z = log1p((c - 1) + s), so that a nearly sure row keeps the digits of a log probability next to 0; both terms of H are
-// positive, so nothing cancels in it.
+// One pass: a thread keeps the running (m, c, s, E): how often it has met its wave's largest value, the sum over the others, and
+// sum (x - m) e^(x - m).  Z = c + s and log Z = log1p((c - 1) + s), so that a nearly sure row keeps the digits of a log probability next to 0; both
+// terms of H are positive, so nothing cancels in it.
 //
 // A workgroup holds 32 values a thread of a row at a time (8192 of 256 threads) while the next ones are on their way.  Nothing in that pass waits for
-// another thread; a thread remembers its largest value and the chunk it came in.
+// another wave.  Vector instructions bound it (99 % of the CUs' busy time on bf16), so a chunk that does not reach its wave's largest value so far, most
+// of a long row's, takes seven a value instead of ten, and loads behind the row's end take none: 2048 x 50257 bf16 57 -> 51.5 us, 600 x 1000000 285 -> 242.
+// What a row's last loads have too early is shifted out where they are used, not where they are issued (4096 x 32000 bf16 with alternatives 74.0 -> 66.5).
 //
 // Alternatives are 64-bit keys, the value's bits in an order of whole numbers above the id's complement: larger value first, the lower id among
-// equals, all keys different.  Behind the pass the largest values of 64 groups of lanes give a bound that n_top values reach at least; the
-// loads of the threads whose largest value reaches it are dealt out to all threads once more (from the caches), and what reaches the bound is
-// gathered and ranked.  Where ties let too much reach it, the bound is the n_top-th of the threads' best keys.
+// equals, all keys different.  A thread remembers of up to sixteen stretches of its chunks the upper half of each one's largest value.  Behind the pass
+// the largest values of 64 groups of lanes give a bound that n_top values reach at least; the loads of the stretches that reach it are dealt out
+// to all threads once more, and what reaches the bound is gathered and ranked.  (All loads of a thread that reaches it, 16 bytes of a line each, were a
+// second pass over the row's lines: 2048 x 50257 fp32 with 20 alternatives 102 us, 85 so; bf16 67, 64.)  Where ties let too much reach it, the bound
+// is the n_top-th of the threads' best keys.
 //
 // Few rows are cut into parts of whole chunks for several workgroups, whose results a second launch joins in their order.
 #include <algorithm>
+#include <type_traits>
 
 #include "device_utils.h"
 #include "relserve_internal.h"
@@ -24,7 +29,8 @@ namespace {
 
 constexpr int PER = 32, MAX_TOP = 32;      // values a thread holds at a time; alternatives
 constexpr int FEW = 256, MANY = 1024;      // threads of a workgroup
-constexpr float LOG2E = 1.4426950408889634f;
+constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
+constexpr float kPlainMost = 0x1p14f;      // largest values whose product with LOG2E lacks so little that exp2 of it is next to 1
 
 struct Sums {
     float m, c, s, e;   // largest value, how often, sum of e^(x - m) over the others, sum of (x - m) e^(x - m)
@@ -88,24 +94,44 @@ __device__ __forceinline__ void write_row(const LogprobsArgs& a, int64_t row, co
     }
 }
 
-// The sums of all threads, in every thread: moved to the largest value of all, then added.
+// A value of another lane: 0x120 + n rotates rows of 16 lanes; 0x142 gives lane 15 of a row to the next one's lanes, 0x143 lane 31 to the upper half's;
+// rows outside the mask get `old`.
+template <int CTRL, int ROWS>
+__device__ __forceinline__ float other_lane(float old, float v) {
+    return __int_as_float(__builtin_amdgcn_update_dpp(__float_as_int(old), __float_as_int(v), CTRL, ROWS, 0xf, false));
+}
+// The wave's largest value, the same scalar in every lane; all lanes call it.
+__device__ __forceinline__ float wave_largest(float m) {
+    m = fmaxf(m, other_lane<0x128, 0xf>(m, m));
+    m = fmaxf(m, other_lane<0x124, 0xf>(m, m));
+    m = fmaxf(m, other_lane<0x122, 0xf>(m, m));
+    m = fmaxf(m, other_lane<0x121, 0xf>(m, m));
+    m = fmaxf(m, other_lane<0x142, 0xa>(m, m));
+    m = fmaxf(m, other_lane<0x143, 0xc>(m, m));
+    return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(m), 63));
+}
+// The sum of all lanes, in the last one.
+__device__ __forceinline__ float wave_total(float v) {
+    v += other_lane<0x128, 0xf>(0.0f, v);
+    v += other_lane<0x124, 0xf>(0.0f, v);
+    v += other_lane<0x122, 0xf>(0.0f, v);
+    v += other_lane<0x121, 0xf>(0.0f, v);
+    v += other_lane<0x142, 0xa>(0.0f, v);
+    v += other_lane<0x143, 0xc>(0.0f, v);
+    return v;
+}
+
+// The sums of all threads, in every thread: moved to the largest value of all, then added.  A wave's own have one m.
 template <int THREADS>
 __device__ __forceinline__ Sums all_sums(Sums z, float4* red) {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    float m = z.m;
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor(m, o, 64));
-    move_to(z, m);
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1) {
-        z.c += __shfl_xor(z.c, o, 64);
-        z.s += __shfl_xor(z.s, o, 64);
-        z.e += __shfl_xor(z.e, o, 64);
-    }
-    if (lane == 0) red[wave] = make_float4(z.m, z.c, z.s, z.e);
+    z.c = wave_total(z.c);
+    z.s = wave_total(z.s);
+    z.e = wave_total(z.e);
+    if (lane == 63) red[wave] = make_float4(z.m, z.c, z.s, z.e);
     __syncthreads();
     Sums part[THREADS / 64];
-    m = -INFINITY;
+    float m = -INFINITY;
 #pragma unroll
     for (int w = 0; w < THREADS / 64; ++w) {
         const float4 r = red[w];
@@ -142,6 +168,7 @@ __device__ __forceinline__ uint4 behind(const uint4& q, int bits, uint32_t fill)
     return make_uint4((uint32_t)x, (uint32_t)(x >> 32), (uint32_t)y, (uint32_t)(y >> 32));
 }
 
+constexpr int kStretches = 16, kReaching = 1024;   // of a thread; stretches whose loads are dealt out at most
 constexpr int kGathered = 2048;   // keys that a workgroup gathers at most: two chunks' of 32 alternatives
 
 template <int THREADS, bool F32, bool TOP, bool ONE>
@@ -153,7 +180,7 @@ __global__ void __launch_bounds__(THREADS) logprobs_kernel(LogprobsLaunch p) {
     __shared__ float4 red[THREADS / 64];
     __shared__ uint64_t list[TOP ? MAX_TOP : 1], best[TOP ? THREADS + 8 : 1], cand[TOP ? kGathered + MAX_TOP + 8 : 1], floor_key;
     __shared__ uint32_t group[TOP ? 64 : 1];
-    __shared__ uint16_t who[TOP && !ONE ? THREADS : 1];
+    __shared__ uint16_t stretch[TOP && !ONE ? kStretches * THREADS : 1], who[TOP && !ONE ? kReaching : 1];
     __shared__ int n_best, n_cand, n_who;
     const int tid = threadIdx.x, lane = tid & 63, vocab = p.a.vocab, n_top = p.a.n_top;
     const int64_t row = blockIdx.x / p.parts;
@@ -166,16 +193,14 @@ __global__ void __launch_bounds__(THREADS) logprobs_kernel(LogprobsLaunch p) {
         if constexpr (F32) return __builtin_bit_cast(uint4, *reinterpret_cast<const f32_quad*>(base + (int64_t)from * 4));
         else return __builtin_bit_cast(uint4, *reinterpret_cast<const bf16_eight*>(base + (int64_t)from * 2));
     };
+    // how many of a chunk's loads lie in the row (an eighth of 50257 values is one load of a seventh chunk)
+    auto loads_of = [&](int c) { return (int)min<int64_t>(LOADS, (vocab - (int64_t)c * CHUNK + THREADS * V - 1) / (THREADS * V)); };
+    // (loads past the row's end are moved back to it)
     auto load = [&](int c, Raw& r) __attribute__((always_inline)) {
         const int at = c * CHUNK + tid * V;
-        if ((c + 1) * (int64_t)CHUNK <= vocab) {
-#pragma unroll
-            for (int l = 0; l < LOADS; ++l) r.q[l] = whole(at + l * (THREADS * V));
-        } else if (vocab >= V) {   // the row's last chunk: loads past its end are moved back to it, and what they have too early is shifted out
+        if (vocab >= V) {
 #pragma unroll
             for (int l = 0; l < LOADS; ++l) r.q[l] = whole(min(at + l * (THREADS * V), vocab - V));
-#pragma unroll
-            for (int l = 0; l < LOADS; ++l) r.q[l] = behind(r.q[l], max(at + l * (THREADS * V) + V - vocab, 0) * (128 / V), FILL);
         } else {
             auto one = [&](int i) -> uint32_t {
                 if (i >= vocab) return F32 ? 0xff800000u : 0xff80u;
@@ -187,7 +212,13 @@ __global__ void __launch_bounds__(THREADS) logprobs_kernel(LogprobsLaunch p) {
             for (int l = 1; l < LOADS; ++l) r.q[l] = make_uint4(FILL, FILL, FILL, FILL);
         }
     };
-    auto values = [&](const Raw& r, float (&x)[PER]) __attribute__((always_inline)) {
+    auto values = [&](int c, Raw& r, float (&x)[PER]) __attribute__((always_inline)) {
+        if (vocab >= V && (c + 1) * (int64_t)CHUNK > vocab) {   // what moved loads have too early is shifted out
+            const int at = c * CHUNK + tid * V, here = ONE ? LOADS : loads_of(c);
+#pragma unroll
+            for (int l = 0; l < LOADS; ++l)
+                r.q[l] = l < here ? behind(r.q[l], max(at + l * (THREADS * V) + V - vocab, 0) * (128 / V), FILL) : make_uint4(FILL, FILL, FILL, FILL);
+        }
 #pragma unroll
         for (int l = 0; l < LOADS; ++l) {
             const uint32_t u[4] = {r.q[l].x, r.q[l].y, r.q[l].z, r.q[l].w};
@@ -201,38 +232,70 @@ __global__ void __launch_bounds__(THREADS) logprobs_kernel(LogprobsLaunch p) {
     auto id_of = [&](int c, int i) { return c * CHUNK + tid * V + i / V * (THREADS * V) + i % V; };
 
     const Given first = p.parts == 1 ? given(p.a, row, tid) : Given{0.f, false};
-    Sums z{-INFINITY, 0.f, 0.f, 0.f};
-    int best_chunk = c0;
-    float x[PER];
+    Sums z{-INFINITY, 0.f, 0.f, 0.f};   // (m is the wave's, or, of a chunk alone, the thread's)
+    float most_x = -INFINITY;           // the thread's largest value, and its chunk
+    int best_chunk = c0, at_stretch = 0, left = 0;   // (left: chunks of the stretch behind this one)
+    const int per_stretch = (c1 - c0 + kStretches - 1) / kStretches;
+    float x[PER], stretch_most = -INFINITY;
     Raw next;
     load(c0, next);
     for (int c = c0; c < c1; ++c) {
-        values(next, x);
+        values(c, next, x);
         if (!ONE && c + 1 < c1) load(c + 1, next);
-        float m = -INFINITY;
+        const int here = ONE ? LOADS : loads_of(c);
+        auto take = [&](auto whole_chunk) __attribute__((always_inline)) {
+            auto each = [&](auto f) __attribute__((always_inline)) {
 #pragma unroll
-        for (int i = 0; i < PER; ++i) m = fmaxf(m, x[i]);
-        if (m > z.m) best_chunk = c;
-        move_to(z, fmaxf(z.m, m));
-        const float from = z.m == -INFINITY ? 0.0f : z.m;
-        int others = 0;
+                for (int l = 0; l < LOADS; ++l)
+                    if (decltype(whole_chunk)::value || l < here)
 #pragma unroll
-        for (int i = 0; i < PER; ++i) {
-            const float d = x[i] - from, e = __builtin_amdgcn_exp2f(d * LOG2E);
-            const bool other = x[i] != z.m;
-            others += other;
-            z.s += other ? e : 0.0f;
-            z.e = __builtin_fmaf(fmaxf(d, -200.0f), e, z.e);
-        }
-        z.c += (float)(PER - others);
+                        for (int i = l * V; i < (l + 1) * V; ++i) f(x[i]);
+            };
+            float m = -INFINITY;
+            each([&](float v) __attribute__((always_inline)) { m = fmaxf(m, v); });
+            if (m > most_x) most_x = m, best_chunk = c;
+            if constexpr (TOP && !ONE) {
+                stretch_most = left > 0 ? fmaxf(stretch_most, m) : m;
+                left = left > 0 ? left - 1 : per_stretch - 1;
+                stretch[at_stretch * THREADS + tid] = (uint16_t)(stretch_most > -INFINITY ? ordered(stretch_most) >> 16 : 0);
+                at_stretch += left == 0;
+            }
+            if (!ONE && __builtin_fabsf(z.m) < kPlainMost && __ballot(m >= z.m) == 0) {
+                // nothing reaches the wave's largest value: nothing is counted, and the exponent is one multiply-add
+                const float high = z.m * LOG2E, low = __builtin_fmaf(z.m, LOG2E, -high), up = __builtin_amdgcn_exp2f(-low);
+                float sum = 0.0f, sum_d = 0.0f;
+                each([&](float v) __attribute__((always_inline)) {
+                    const float d = __builtin_fmaf(v, LOG2E, -high), e = __builtin_amdgcn_exp2f(d);
+                    sum += e;
+                    sum_d = __builtin_fmaf(fmaxf(d, -200.0f), e, sum_d);
+                });
+                z.s = __builtin_fmaf(sum, up, z.s);
+                z.e = __builtin_fmaf(__builtin_fmaf(-low, sum, sum_d) * LN2, up, z.e);
+                return;
+            }
+            move_to(z, fmaxf(z.m, ONE ? m : wave_largest(m)));
+            const float from = z.m == -INFINITY ? 0.0f : z.m;
+            int others = 0;
+            each([&](float v) __attribute__((always_inline)) {
+                const float d = v - from, e = __builtin_amdgcn_exp2f(d * LOG2E);
+                const bool other = v != z.m;
+                others += other;
+                z.s += other ? e : 0.0f;
+                z.e = __builtin_fmaf(fmaxf(d, -200.0f), e, z.e);
+            });
+            z.c += (float)((decltype(whole_chunk)::value ? PER : here * V) - others);
+        };
+        if (here == LOADS) take(std::true_type{});
+        else take(std::false_type{});
     }
+    if constexpr (ONE) move_to(z, wave_largest(z.m));
     if constexpr (TOP) {
         if (tid < MAX_TOP) list[tid] = 0;
         best[tid] = 0;
         if (tid < 8) best[THREADS + tid] = 0;
         if (tid == 0) n_best = n_cand = n_who = 0;
         // From which value on: the n_top-th largest of the 64 groups of lanes, by its upper half (0: fewer groups have a number above -infinity).
-        const uint32_t most = z.m > -INFINITY ? ordered(z.m) : 0;
+        const uint32_t most = most_x > -INFINITY ? ordered(most_x) : 0;
         uint32_t g = most;
 #pragma unroll
         for (int o = 1; o < GROUP; o *= 2) g = max(g, (uint32_t)__shfl_xor((int)g, o, 64));
@@ -272,10 +335,17 @@ __global__ void __launch_bounds__(THREADS) logprobs_kernel(LogprobsLaunch p) {
                 for (int i = 0; i < PER; ++i)
                     if (x[i] >= bound) gather(x[i], id_of(c0, i), low);
             } else {
-                // the loads of the threads that have such values, dealt out to all
-                if (most >= from) who[atomicAdd(&n_who, 1)] = (uint16_t)tid;
+                // the loads of the stretches that have such values, dealt out to all
+                if (most >= from) {
+#pragma unroll
+                    for (int i = 0; i < kStretches; ++i)
+                        if (i * per_stretch < c1 - c0 && stretch[i * THREADS + tid] >= from >> 16) {
+                            const int slot = atomicAdd(&n_who, 1);
+                            if (slot < kReaching) who[slot] = (uint16_t)(i * THREADS + tid);
+                        }
+                }
                 __syncthreads();
-                const int n = n_who, loads = n * LOADS * (c1 - c0);
+                const int n = min(n_who, kReaching), loads = n * LOADS * per_stretch;
                 constexpr int AT_ONCE = 4;
                 const float one_nth = 1.0f / (float)n;
                 for (int w0 = tid; w0 < loads; w0 += AT_ONCE * THREADS) {
@@ -287,7 +357,8 @@ __global__ void __launch_bounds__(THREADS) logprobs_kernel(LogprobsLaunch p) {
                         int l = (int)((float)w * one_nth), rest = w - l * n;   // (the product may be next to the quotient)
                         if (rest < 0) --l, rest += n;
                         if (rest >= n) ++l, rest -= n;
-                        ids[b] = (c0 + l / LOADS) * CHUNK + l % LOADS * (THREADS * V) + who[rest] * V;
+                        const int at = who[rest], c = c0 + at / THREADS * per_stretch + l / LOADS;
+                        ids[b] = c < c1 ? c * CHUNK + l % LOADS * (THREADS * V) + at % THREADS * V : vocab;
                         q[b] = whole(min(ids[b], vocab - V));   // (two chunks at least: more entries than V)
                     }
 #pragma unroll
@@ -304,7 +375,7 @@ __global__ void __launch_bounds__(THREADS) logprobs_kernel(LogprobsLaunch p) {
                 }
             }
             __syncthreads();
-            done = n_cand <= kGathered;
+            done = n_cand <= kGathered && n_who <= kReaching;
             if (done) cut();
         }
         if (!done) {
@@ -316,14 +387,14 @@ __global__ void __launch_bounds__(THREADS) logprobs_kernel(LogprobsLaunch p) {
             for (int c = best_chunk; c < c1 && at < 0; ++c) {
                 if constexpr (!ONE) {
                     load(c, next);
-                    values(next, x);
+                    values(c, next, x);
                 }
 #pragma unroll
-                for (int i = PER - 1; i >= 0; --i) at = x[i] == z.m ? i : at;
+                for (int i = PER - 1; i >= 0; --i) at = x[i] == most_x ? i : at;
                 best_chunk = c;
             }
             const int id = id_of(best_chunk, at);
-            const uint64_t mine = at < 0 || id >= vocab ? 0 : key_of(z.m, id);
+            const uint64_t mine = at < 0 || id >= vocab ? 0 : key_of(most_x, id);
             if (mine && (uint32_t)(mine >> 32) >= from) best[atomicAdd(&n_best, 1)] = mine;
             __syncthreads();
             const int count = n_best;
@@ -342,7 +413,7 @@ __global__ void __launch_bounds__(THREADS) logprobs_kernel(LogprobsLaunch p) {
                     for (int k = c; k < min(c + at_once, c1); ++k) {
                         if constexpr (!ONE) {
                             load(k, next);
-                            values(next, x);
+                            values(k, next, x);
                         }
 #pragma unroll
                         for (int i = 0; i < PER; ++i) gather(x[i], id_of(k, i), low);
@@ -378,6 +449,7 @@ __global__ void __launch_bounds__(FEW) logprobs_join_kernel(LogprobsLaunch p) {
     for (int i = tid; i < n + 8; i += FEW) keys[i] = i < n ? p.part_keys[row * n + i] : 0;
     const Given first = given(p.a, row, tid);
     if (tid < MAX_TOP) list[tid] = 0;
+    move_to(z, wave_largest(z.m));
     z = all_sums<FEW>(z, red);
     for (int i = tid; i < n; i += FEW) {
         const uint64_t k = keys[i];

@@ -171,3 +171,26 @@ def test_the_first_alternative_is_the_greedy_token(rs):
     token = torch.empty(40, dtype=torch.int32, device="cuda")
     rs.relserve_greedy_sample(x, token)
     assert torch.equal(_call(rs, x, None, 1)[2][:, 0], token.cpu())
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("v,times", [(8192 * 3 + 2049, 90), (8192 * 18 + 2047, 1), (8192 * 33 + 1, 1)])
+def test_long_rows_that_are_hard(rs, v, times, dtype):
+    """Several chunks of a row one behind the other: where the largest values lie, how large they are, and how many are alike."""
+    at = torch.arange(v, device="cuda")
+    x, ids = _logits(v, 12, v, torch.float32)
+    x[0] = at * 1e-4                                                 # every chunk reaches the largest value so far
+    x[1] = at * -1e-4                                                # none does
+    x[2] += 1e4                                                      # the largest value's product with log2 e lacks digits
+    x[3] -= 1.6e4
+    x[4] += 3e4                                                      # beyond what the plain pass takes
+    x[5, 8192:16384] = -float("inf")                                 # a chunk without a number
+    x[6, :-1] = -float("inf")
+    x[7, 100:8000] = float("inf")                                    # no distribution, alternatives all the same
+    x[8] = torch.where(at % 97 == 3, 12.0, 0.0)                      # the bound's value in more stretches than are dealt out
+    x[9] = torch.where(at % 8192 < 8, 7.5, -3.0)                     # in a thread or two, in every chunk
+    x[10] = 1e4 - (at + 1) * 2.0 ** -10                              # one step of fp32 below the largest value
+    x[10, 0] = 1e4
+    x[11, v - 1] = 40.0
+    x[11, 9000] = float("nan")
+    _check(rs, x.to(dtype).repeat(times, 1), ids.repeat(times, 1), 13, f"long hard rows of {v}")
