@@ -259,12 +259,18 @@ __global__ void __launch_bounds__(64 * WM * WN) tile_kernel(Args p) {
     // stage's last operands are in registers ahead of that pair: there the wave waits for the next stage and hands this one over, reads the next
     // step's first operands beside the last products and refills the stage beside the next step's.  A product's results are added two products
     // later, those of a step's last two beside the next step's first.
-    constexpr int NM = TN * TM, HAND = NM - 2 * TM, LAG = 2, NB = TN == 8 ? 3 : TN;
+    constexpr int NM = TN * TM, HAND = NM - 2 * TM, LAG = 2, NB = WIDE ? 2 : TN == 8 ? 3 : TN;
     static_assert(NM % 4 == 0 && (TN == 4 || TN == 8) && LAG <= TM, "a ring of four results, products for all tokens' scales behind the hand-over");
     constexpr auto frag_of = [](int j) { return j < HAND ? j / TM : TN - 2 + (j - HAND) % 2; };
     constexpr auto token_of = [](int j) { return j < HAND ? j % TM : (j - HAND) / 2; };
     // registers of fragment f: the last two and the first one of the next step are held together, and neighbours
-    constexpr auto buffer_of = [](int f) { constexpr int of8[8] = {2, 0, 1, 0, 1, 2, 0, 1}; return TN == 8 ? of8[f] : f; };
+    constexpr auto buffer_of = [](int f) { constexpr int of8[8] = {2, 0, 1, 0, 1, 2, 0, 1}; return WIDE ? f / 3 : TN == 8 ? of8[f] : f; };
+    // Widening: the 16 conversions of a fragment behind one product, those of the next a product or two later, once the registers they go to are free and
+    // BEHIND products after the fragment's read (all of them ahead of their first products: 2000 x 8192 x 8192 243 us, so 239; none at all, in a
+    // build that leaves them out, 20 % less).  wide_of: fragment f's registers.
+    static_assert(!WIDE || TN == 4, "widened fragments of features");
+    constexpr int BEHIND = TM > 2 ? 2 : 1, NA = WIDE ? 2 : TM;
+    constexpr auto wide_of = [](int f) { return f < 3 ? f : 1; };
     using operand_t = decltype(operand<WIDE>(i32x8_t{}));
     f32x4_t acc[TN][TM], sum[4];
 #pragma unroll
@@ -273,8 +279,8 @@ __global__ void __launch_bounds__(64 * WM * WN) tile_kernel(Args p) {
         for (int i = 0; i < TM; ++i) acc[f][i] = f32x4_t{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int q = 0; q < 4; ++q) sum[q] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-    i32x8_t w_raw[NB], a_raw[TM];          // as read
-    operand_t wf[WIDE ? 2 : 1], af[WIDE ? TM : 1];   // widened
+    i32x8_t w_raw[NB], a_raw[NA];          // as read
+    operand_t wf[WIDE ? 3 : 1], af[WIDE ? TM : 1];   // widened
     float ts[TM], tn[TM], wn0 = 0.f, wn1 = 0.f;   // tokens' scales times the weights' of the features in turn; the tokens' and the weights' as read
 #pragma unroll
     for (int i = 0; i < TM; ++i) ts[i] = tn[i] = 0.f;
@@ -307,13 +313,20 @@ __global__ void __launch_bounds__(64 * WM * WN) tile_kernel(Args p) {
             const int since = j >= HAND ? j - HAND : j - HAND + NM;
             if ((j >= HAND ? BEGIN : REST) && since % GAP == 0 && since / GAP < LOADS) load(since / GAP);
             if constexpr (WIDE) {
-                if (f == 0) af[i] = operand<WIDE>(a_raw[i]);
-                if (j < HAND ? i == 0 : j < HAND + 2) wf[f % 2] = operand<WIDE>(w_raw[buffer_of(f)]);
-                sum[j % 4] = block_sum(wf[f % 2], af[i]);
+                sum[j % 4] = block_sum(wf[wide_of(f)], af[i]);
             } else {
                 sum[j % 4] = block_sum(w_raw[buffer_of(f)], a_raw[i]);
             }
             __builtin_amdgcn_sched_barrier(0);
+            if constexpr (WIDE) {
+                if (j == TM - (TM > 2 ? 2 : 1)) wf[1] = operand<WIDE>(w_raw[buffer_of(1)]);
+                if (j == TM + BEHIND) wf[2] = operand<WIDE>(w_raw[buffer_of(2)]);
+                if (j == HAND) wf[1] = operand<WIDE>(w_raw[buffer_of(3)]);
+                if (j == HAND + 2) wf[0] = operand<WIDE>(w_raw[buffer_of(0)]);   // the next step's
+#pragma unroll
+                for (int q = 0; q < TM; ++q)
+                    if (j == (HAND + 2 * q + 1 + BEHIND) % NM) af[q] = operand<WIDE>(a_raw[q % NA]);
+            }
             if (j < HAND) {   // the next fragment of features; behind the last but two both that remain
                 if (i == 0) w_raw[buffer_of(f + 1)] = read(wa, w_dist(f + 1));
                 if (f == TN - 3 && i == TM / 2) w_raw[buffer_of(TN - 1)] = read(wa, w_dist(TN - 1));
@@ -323,7 +336,7 @@ __global__ void __launch_bounds__(64 * WM * WN) tile_kernel(Args p) {
                     asm("" : "+v"(na.lo), "+v"(na.hi));
                     w_raw[buffer_of(0)] = read(At{w_at + next, (w_at ^ 64) + next}, 0);
                 }
-                if ((j - HAND) % 2) a_raw[i] = read(na, 16 * KB * i);
+                if ((j - HAND) % 2) a_raw[i % NA] = read(na, 16 * KB * i);
             }
             if (j == LAG || (SWI && j == TN / 2 * TM + LAG)) {
 #pragma unroll
@@ -354,10 +367,12 @@ __global__ void __launch_bounds__(64 * WM * WN) tile_kernel(Args p) {
     __syncthreads();
 #pragma unroll
     for (int i = 0; i < TM; ++i) {
-        a_raw[i] = read(At{a_at, a_at ^ 64}, 16 * KB * i);
+        a_raw[i % NA] = read(At{a_at, a_at ^ 64}, 16 * KB * i);
+        if constexpr (WIDE) af[i] = operand<WIDE>(a_raw[i % NA]);
         tn[i] = *(lds_float)(uintptr_t)(ts_at + 64 * i);
     }
     w_raw[buffer_of(0)] = read(At{w_at, w_at ^ 64}, 0);
+    if constexpr (WIDE) wf[0] = operand<WIDE>(w_raw[buffer_of(0)]);
     wn0 = *(lds_float)(uintptr_t)ws_at;
     if (SWI) wn1 = *(lds_float)(uintptr_t)(ws_at + 4);
     const std::true_type yes;
