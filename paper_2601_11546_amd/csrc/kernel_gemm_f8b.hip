@@ -643,14 +643,15 @@ struct Plan { int tile, splits; };
 enum { ROWS_16, ROWS_16_NARROW, ROWS_32, ROWS_32_NARROW, ROWS_64, TILE_64, TILE_128, TILE_128_WIDE, TILE_256, PLANS };
 
 // What a tile takes, in us: a launch's base, then for each round of workgroups over the chip its begin and end and its k steps (of a wave's own slices
-// for rows), of codes and of codes widened to bf16; a step of a round that leaves CUs idle costs `alone` of that, the rest by how many work.
-// Fitted to 4200 measured launches of 129 shapes (1 .. 8192 tokens, weights from memory): the plans chosen by it are 2.7 % slower than the best one of
-// each shape on average, 37 % at worst (700 x 612 x 2560: 15.6 us for 11.4).
-struct TileCost { int rows, features, at_once; double base, step, step_wide, round, alone; };
+// for rows), both of codes and of codes widened to bf16; a step of a round that leaves CUs idle costs `alone` of that, the rest by how many work.
+// Fitted to measured launches, weights from memory: 4200 of 129 shapes of 1 .. 8192 tokens, and for widened codes 2700 of 116 shapes of 33 .. 4099.  The
+// plans chosen by it are 2.7 % slower than the best one of each shape on average, 37 % at worst (700 x 612 x 2560: 15.6 us for 11.4); of the
+// second set 0.9 % and 16 % (128 x 5120 x 5120 onto fp32: 22.4 us for 19.2).
+struct TileCost { int rows, features, at_once; double base, step, step_wide, round, round_wide, alone; };
 constexpr TileCost kCost[PLANS] = {
-    {16, 32, 512, 0.11, 1.17, 0.79, 1.63, 0.19},  {16, 16, 768, 0.14, 0.53, 5.66, 1.29, 0.18},  {32, 32, 512, 2.45, 1.52, 1.15, 1.22, 0.10},
-    {32, 16, 512, 0.15, 0.056, 0.45, 0.57, 0.27}, {64, 32, 256, 2.08, 0.68, 0.70, 2.14, 0.68},  {64, 128, 512, 1.62, 0.80, 1.10, 4.12, 0.74},
-    {128, 128, 512, 3.42, 1.50, 1.53, 4.50, 2.37}, {128, 256, 256, 2.38, 0.91, 1.62, 12.0, 0.53}, {256, 256, 256, 0.0, 1.70, 2.40, 16.2, 0.72}};
+    {16, 32, 512, 0.11, 1.17, 0.79, 1.63, 1.63, 0.19},  {16, 16, 768, 0.14, 0.53, 5.66, 1.29, 1.29, 0.18},  {32, 32, 512, 2.45, 1.52, 0.94, 1.22, 0.78, 0.10},
+    {32, 16, 512, 0.15, 0.056, 0.45, 0.57, 0.57, 0.27}, {64, 32, 256, 2.08, 0.68, 0.66, 2.14, 1.12, 0.68},  {64, 128, 512, 1.62, 0.80, 0.93, 4.12, 3.40, 0.74},
+    {128, 128, 512, 3.42, 1.50, 1.38, 4.50, 4.67, 2.37}, {128, 256, 256, 2.38, 0.91, 1.38, 12.0, 5.16, 0.53}, {256, 256, 256, 0.0, 1.70, 2.40, 16.2, 16.2, 0.72}};
 constexpr int64_t kSlabFloats = (int64_t)1 << 24;   // of partial sums: 64 MB, which the last-level cache holds
 
 double cost_of(const Args& p, bool wide, int tile, int splits) {
@@ -658,7 +659,7 @@ double cost_of(const Args& p, bool wide, int tile, int splits) {
     const double units = (double)((p.T + c.rows - 1) / c.rows) * ((p.N + c.features - 1) / c.features) * splits, rounds = units / c.at_once;
     const double steps = (double)((p.K / KB + splits - 1) / splits) / (tile <= ROWS_64 ? 4 : 1);
     const double busy = rounds > 1 ? 1.0 : c.alone + (1.0 - c.alone) * rounds;
-    const double work = std::max(1.0, std::ceil(rounds)) * (c.round + (wide ? c.step_wide : c.step) * steps * busy);
+    const double work = std::max(1.0, std::ceil(rounds)) * (wide ? c.round_wide + c.step_wide * steps * busy : c.round + c.step * steps * busy);
     // operands from memory and, for each column of tiles, from the caches
     const double bytes = (double)p.N * p.K + 0.02 * (double)p.T * p.K * ((p.N + c.features - 1) / c.features), out = (double)p.T * p.N;
     return c.base + std::max(work, bytes / 4.5e6) + (splits > 1 ? 2.0 + splits * out * 4 / 6e6 + out * 6 / 5e6 : out * 4 / 20e6);
