@@ -739,8 +739,8 @@ hipError_t run(const Args& p, hipStream_t s) { return run_plan<EPI>(p, plan_for(
 
 }  // namespace
 
-// (grows with either size, so that the largest call's serves all)
-int64_t gemm_f8b_scratch_floats(int64_t T, int64_t N) { return std::max<int64_t>(64, std::min(16 * T * N, kSlabFloats)); }
+// (grows with either size, so that the largest call's serves all; any 32-bit sizes, whose product has up to 62 bits)
+int64_t gemm_f8b_scratch_floats(int64_t T, int64_t N) { return std::max<int64_t>(64, 16 * std::min(T * N, kSlabFloats / 16)); }
 
 GemmPlanF8b gemm_plan_f8b(int32_t T, int32_t N, int32_t K, int32_t epilogue, bool scratch) {
     float some_scratch;
