@@ -276,13 +276,16 @@ __global__ void __launch_bounds__(THREADS) logprobs_kernel(LogprobsLaunch p) {
             move_to(z, fmaxf(z.m, ONE ? m : wave_largest(m)));
             const float from = z.m == -INFINITY ? 0.0f : z.m;
             int others = 0;
+            float sum = 0.0f, sum_e = 0.0f;   // of the chunk, as above: a chain through all of a thread's values drifts with equal ones
             each([&](float v) __attribute__((always_inline)) {
                 const float d = v - from, e = __builtin_amdgcn_exp2f(d * LOG2E);
                 const bool other = v != z.m;
                 others += other;
-                z.s += other ? e : 0.0f;
-                z.e = __builtin_fmaf(fmaxf(d, -200.0f), e, z.e);
+                sum += other ? e : 0.0f;
+                sum_e = __builtin_fmaf(fmaxf(d, -200.0f), e, sum_e);
             });
+            z.s += sum;
+            z.e += sum_e;
             z.c += (float)((decltype(whole_chunk)::value ? PER : here * V) - others);
         };
         if (here == LOADS) take(std::true_type{});
