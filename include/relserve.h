@@ -416,8 +416,11 @@ int32_t relserve_layer_step_i8(const relserve_layer* layer, const relserve_batch
  * relserve_linear_f8b: out[t, n] = sum over blocks b of k of (sum over k in b of a[t, k] * w[n, k]) * (a_scale[b, t] * w_scale[n / 128, b]) on codes, a
  * block's sum added with one fused multiply-add in fp32; epilogues, residuals and outputs as relserve_linear (0 and 3 read no residual).
  * For fp32 outputs (epilogue 1) a block's products are exact and its sum is one of fp32: codes are multiplied as bf16 values.  bf16 outputs use the
- * matrix instruction on 8-bit codes, which drops what lies some 14 bits below the largest of a few neighbouring products: they are off by up to 2e-5 of a
- * row's norm beside their own rounding.
+ * matrix instruction on 8-bit codes, which cuts each product off, towards zero, at 2^-13 of 2^E, E the largest sum of two codes' exponents among the products of
+ * eight consecutive k (of subnormal codes -6).  Beside their own rounding (2^-9 of each value on average) they are off by at most 2^-10 of what the
+ * products' magnitudes add up to where the largest products are of normal codes; of the result's norm by 1.4e-5 on normal values, 2e-5 where a few
+ * channels are eight times as large (single rows 4e-5), 6e-5 where magnitudes spread over orders of magnitude, so that one output in a hundred (three in
+ * a hundred) is the neighbouring number of bf16.
  * K a multiple of 128, N of 4 (of 16 for SwiGLU), T K and N K below 2^31 (RELSERVE_ERR_TOO_LARGE).  With SwiGLU the gate's and the up's rows are blocked
  * each from their own first one: w_scale [2 ceil(N / 256), K / 128].  packed != 0: w is relserve_pack_weight applied to the matrix seen as [N, K / 2]
  * two-byte units.  workspace: scratch as in relserve_layer_step, of at least relserve_linear_f8b_workspace_bytes(T, N) bytes (64 MB at most, growing

@@ -1,0 +1,221 @@
+"""What the block-scaled projections lose before an output is rounded to bf16, against 64-bit arithmetic.
+
+The matrix instruction on 8-bit codes takes the products of eight consecutive k together and cuts each one off, towards zero, at 2^-13 of 2^E, E the
+largest sum of two codes' exponents among them (of subnormal codes that of the smallest normal ones, -6); what is left is added in fp32.  A product of two codes has
+three bits of mantissa a factor, so that only those are cut whose exponents lie more than seven below E.  CUT is what the formula of the header becomes by that,
+in 64 bits; the kernels are off from it by roundings of fp32 (U = 2^-24) alone, and from the formula by what each family of values gives.
+"""
+import pytest
+import torch
+
+from tests import f8b_paths
+
+pytestmark = pytest.mark.gpu
+
+U, B = 2.0 ** -24, 2.0 ** -8
+CODE = torch.float8_e4m3fn
+
+
+@pytest.fixture(scope="module")
+def rs():
+    from paper_2601_11546_amd import binding
+    return binding
+
+
+def _gen(seed):
+    g = torch.Generator(device="cuda")
+    g.manual_seed(seed)
+    return g
+
+
+def _randn(g, *size):
+    return torch.randn(*size, generator=g, device="cuda", dtype=torch.float32)
+
+
+def _codes(rs, v, rows):
+    t, n = v.shape
+    c = torch.empty(t, n, dtype=CODE, device="cuda")
+    s = torch.empty(*((-(-t // 128), n // 128) if rows == 128 else (n // 128, t)), device="cuda")
+    rs.relserve_quantise_f8b(v.to(torch.bfloat16), c, s, block_rows=rows)
+    return c, s
+
+
+# what the cut is of a whole result's norm, at most (the cut formula on such values: normal 1.4e-5, channels 2.1e-5, spread 6.2e-5, random codes 5.6e-5:
+# rounded up by some fifth)
+FAMILIES = {"normal": 1.7e-5, "channels": 2.6e-5, "spread": 7.5e-5, "codes": 7e-5}
+# ... and of a single row's, whatever its values, if they are no subnormal codes: seven products of a group lose less than 2^(E - 13) each, evenly spread and of either sign,
+# 7 / 3 * 4^(E - 13) of its variance; the group's largest product alone is 2^E or more, so that all groups' squares add up to 4^E or more each
+ROW = (7 / 3) ** 0.5 * 2.0 ** -13
+
+
+def _problem(rs, g, family, t, n, k, epilogue):
+    """normal values; every 61st channel eight times as large; magnitudes over orders of magnitude; any codes at all under any scales"""
+    half = n // 2 if epilogue == 3 else n
+    if family == "codes":
+        a, w = (torch.randint(0, 256, (r, k), generator=g, device="cuda", dtype=torch.uint8) for r in (t, n))
+        for c in (a, w):
+            c[(c & 127) == 127] = 0
+            c[(c & 127) > 100] &= 0xdf
+        a_scale = torch.exp(_randn(g, k // 128, t)) * 1e-3
+        w_scale = torch.exp(_randn(g, n // half * -(-half // 128), k // 128)) * (1e-3 / k ** 0.5)
+        return a.view(CODE), a_scale, w.view(CODE), w_scale
+    x = _randn(g, t, k)
+    if family == "channels":
+        x[:, ::61] *= 8.0
+    if family == "spread":
+        x *= torch.exp(2.0 * _randn(g, t, k))
+    parts = [_codes(rs, _randn(g, half, k) * 0.02, 128) for _ in range(n // half)]
+    return *_codes(rs, x, 1), torch.cat([p[0].view(torch.uint8) for p in parts]).view(CODE), torch.cat([p[1] for p in parts])
+
+
+def _values(p, epilogue):
+    """codes and scales of every row's blocks, in 64 bits"""
+    a, a_scale, w, w_scale = p
+    n = w.shape[0]
+    half = n // 2 if epilogue == 3 else n
+    row = torch.arange(n, device="cuda")
+    block = torch.where(row < half, row // 128, -(-half // 128) + (row - half) // 128)
+    return a.double(), a_scale.double().t(), w.double(), w_scale.double()[block]
+
+
+def _exact(a, a_scale, w, w_scale):
+    av, wv = a * a_scale.repeat_interleave(128, 1), (w * w_scale.repeat_interleave(128, 1)).t().contiguous()
+    return av @ wv, av.abs() @ wv.abs()
+
+
+def _exponent(codes):
+    return torch.where(codes == 0, -60, torch.frexp(codes)[1].double() - 1).clamp(min=-6)
+
+
+def _cut(a, a_scale, w, w_scale):
+    """the formula on products that are cut off: a few rows and features at a time"""
+    t, k = a.shape
+    y = torch.zeros(t, w.shape[0], dtype=torch.float64, device="cuda")
+    ea, ew = _exponent(a), _exponent(w)
+    for b in range(k // 128):
+        s = slice(128 * b, 128 * b + 128)
+        p = (a[:, None, s] * w[None, :, s]).unflatten(2, (16, 8))
+        e = torch.where(p == 0, -100.0, (ea[:, None, s] + ew[None, :, s]).unflatten(2, (16, 8))).amax(3, keepdim=True)
+        step = torch.exp2(e - 13)
+        y += (torch.trunc(p / step) * step).sum((2, 3)) * a_scale[:, b, None] * w_scale[None, :, b]
+    return y
+
+
+def _linear(rs, p, epilogue, residual=None):
+    a, a_scale, w, w_scale = p
+    t, n = a.shape[0], w.shape[0]
+    out = torch.empty(t, n // 2 if epilogue == 3 else n, dtype=torch.float32 if epilogue == 1 else torch.bfloat16, device="cuda")
+    ws = torch.empty(max(256, rs.relserve_linear_f8b_workspace_bytes(t, n)), dtype=torch.uint8, device="cuda")
+    rs.relserve_linear_f8b(a, a_scale, w, w_scale, epilogue, residual, out, workspace=ws)
+    return out.double()
+
+
+def _some(count, most):
+    return torch.arange(count, device="cuda") if count <= most else torch.unique(torch.linspace(0, count - 1, most, device="cuda").long())
+
+
+SIZES = [(1, 1024, 128), (16, 1024, 5120), (24, 1536, 5120), (64, 1024, 1152), (100, 1024, 8192), (200, 1024, 2048), (333, 1004, 1152), (600, 2048, 1024),
+         (700, 2304, 128), (1282, 1024, 13824), (2050, 2048, 512)]
+
+
+@pytest.mark.parametrize("family", FAMILIES)
+@pytest.mark.parametrize("t,n,k", SIZES)
+def test_before_the_rounding(rs, t, n, k, family):
+    """A residual of minus the result leaves what the product is off by, of which the rounding to bf16 is next to nothing."""
+    print(f"[case] precision {family} {t} x {n} x {k}", flush=True)
+    p = _problem(rs, _gen(t + n + k), family, t, n, k, 2)
+    v = _values(p, 2)
+    y, size = _exact(*v)
+    minus = (-y).float()
+    off = _linear(rs, p, 2, minus) - (y + minus.double())
+    assert float(off.norm() / y.norm()) <= FAMILIES[family]
+    assert float((off.norm(dim=1) / y.norm(dim=1)).max()) <= ROW
+    # ... and that is the cut, to fp32: of a block's 16 groups and 128 products twice a rounding each at most, of a block and of the residual one; bf16's of `off`
+    i, j = _some(t, 24), _some(n, 96)
+    cut = _cut(v[0][i], v[1][i], v[2][j], v[3][j])
+    at = (i[:, None], j[None, :])
+    tol = ((2 * 144 + k // 128 + 8) * U) * size[at] + B * off[at].abs()
+    assert bool(((off[at] - (cut - y[at])).abs() <= tol).all()), float(((off[at] - (cut - y[at])).abs() / tol).max())
+
+
+@pytest.mark.parametrize("size", [s for s in f8b_paths.SIZES if s[3] != 1], ids=str)
+def test_paths(rs, size):
+    """Every tile's outputs in bf16: each one a rounding of the formula on cut products, off by fp32's roundings alone."""
+    t, n, k, epilogue = size
+    print(f"[case] precision of {f8b_paths.SIZES[size]}: {size}", flush=True)
+    g = _gen(t + n + k)
+    p = _problem(rs, g, "codes", t, n, k, epilogue)
+    residual = _randn(g, t, n) if epilogue == 2 else None
+    out = _linear(rs, p, epilogue, residual)
+    v = _values(p, epilogue)
+    i = _some(t, 24)
+    j = _some(n // 2 if epilogue == 3 else n, 96)
+    both = torch.cat([j, j + n // 2]) if epilogue == 3 else j
+    part = v[0][i], v[1][i], v[2][both], v[3][both]
+    y, size_ = _cut(*part), _exact(*part)[1]
+    tol = ((2 * 144 + k // 128 + 8) * U) * size_
+    if residual is not None:
+        y = y + residual[i[:, None], j[None, :]].double()
+        tol = tol + U * y.abs()
+    if epilogue == 3:
+        m = len(j)
+        gate, up, tg, tu = y[:, :m], y[:, m:], tol[:, :m], tol[:, m:]
+        y = gate * torch.sigmoid(gate) * up
+        tol = 1.1 * tg * (up.abs() + tu) + (gate.abs() + tg) * tu + 8 * U * y.abs()    # |silu'| <= 1.1; the exponential, the reciprocal and two products
+    got = out[i[:, None], j[None, :]]
+    low, high = ((y + d).to(torch.bfloat16).double() for d in (-tol, tol))
+    bad = (got < low) | (got > high)
+    assert not bool(bad.any()), f"{int(bad.sum())} of {bad.numel()}"
+
+
+@pytest.mark.parametrize("family", FAMILIES)
+@pytest.mark.parametrize("t,n,k", [(7, 1536, 5120), (60, 2048, 1024), (300, 1536, 2048), (1282, 2560, 1024)])
+def test_swiglu(rs, t, n, k, family):
+    """Outputs of SwiGLU: with d the values' errors before the rounding and s its steps of at most 2^-7 of a value, s |d| is what a rounding on the other side adds to the square of
+    the norm on average, and the sum of s |d| is at most the product of both norms."""
+    print(f"[case] precision swiglu {family} {t} x {n} x {k}", flush=True)
+    p = _problem(rs, _gen(t + n + k), family, t, n, k, 3)
+    y, _ = _exact(*_values(p, 3))
+    if family != "codes":       # gates of a few units
+        y = y / (scale := float(y.std()) / 2)
+        p = (p[0], p[1] / scale, *p[2:])
+        y, _ = _exact(*_values(p, 3))
+    gate, up = y[:, :n // 2], y[:, n // 2:]
+    off = 1.5 * FAMILIES[family]     # of single rows
+    dg, du = (off * v.square().mean(1, keepdim=True).sqrt() for v in (gate, up))
+    want = gate * torch.sigmoid(gate) * up
+    d = ((1.1 * up * dg).square() + (gate * torch.sigmoid(gate) * du).square() + (8 * U * want).square()).sum().sqrt()
+    apart = (_linear(rs, p, 3) - want.to(torch.bfloat16).double()).norm()
+    assert float(apart) <= float((2 * B * want.norm() * d).sqrt())
+
+
+@pytest.mark.parametrize("t", [1, 24, 60, 200, 700, 1300])
+def test_one_large_product_among_small_ones(rs, t):
+    """The largest loss: seven products just under the cut beside one of the smallest mantissa, nearly 7 x 2^-13 of their sum."""
+    n, k = 512, 128
+    a, w = torch.ones(t, k, device="cuda"), torch.zeros(n, k, device="cuda")
+    a[:, 0], w[:, 0] = 256.0, 256.0
+    small = torch.arange(1, 113, device="cuda", dtype=torch.uint8).view(CODE).float()
+    w[:, 1:8] = small[torch.arange(n, device="cuda") % 112][:, None]
+    w[n // 2:] *= -1
+    w[:, 8:16] = 0.5                                            # a group of its own: whole
+    p = a.to(CODE), torch.ones(1, t, device="cuda"), w.to(CODE), torch.ones(4, 1, device="cuda")
+    v = _values(p, 2)
+    y, cut = _exact(*v)[0], _cut(*v)
+    assert float((y - cut).abs().max()) == 7 * 7.5               # (the largest code below 2^(16 - 13) = 8)
+    # (whole numbers and quarters below 2^18, added without a rounding)
+    minus = torch.full((t, n), -2.0 ** 16, device="cuda")
+    minus[:, n // 2:] *= -1
+    assert torch.equal(_linear(rs, p, 2, minus), (cut + minus.double()).to(torch.bfloat16).double())
+
+
+@pytest.mark.parametrize("t,n,k", SIZES)
+def test_fp32_outputs(rs, t, n, k):
+    """Onto fp32 no product is cut: roundings of fp32 alone, each at most U of what has been added so far, 5 a block (four groups of 32 products and the block's)."""
+    print(f"[case] precision fp32 {t} x {n} x {k}", flush=True)
+    for family in ("channels", "codes"):
+        p = _problem(rs, _gen(t + n + k), family, t, n, k, 1)
+        y, _ = _exact(*_values(p, 1))
+        off = _linear(rs, p, 1) - y
+        # errors of roundings are as often up as down: those of a chain of k / 128 sums, each as large as the result so far, and those within the blocks
+        assert float(off.norm() / y.norm()) <= U * (1 + (5 + k / 128) ** 0.5)
