@@ -432,7 +432,7 @@ def _dense(where: str, *tensors, device=None) -> None:
             if device is not None:
                 raise ValueError(f"{where}: {name} lies on {t.device}, other tensors elsewhere")
             device = at
-    if device < 0 or device != torch._C._cuda_getDevice():   # (a tensor on a device: the runtime is up)
+    if device < 0 or device != torch.cuda.current_device():
         raise ValueError(f"{where}: the tensors do not lie on the current device")
 
 
@@ -589,7 +589,7 @@ def relserve_linear_f8b(a, a_scale, w, w_scale, epilogue: int, residual, out, n:
     blocks of 128 rows (with epilogue 3 of the gate's and then of the up's) x 128.  residual: bf16 (epilogue 1, or None) or fp32 (2); the others take None.
     workspace: uint8 tensor of relserve_linear_f8b_workspace_bytes(T, N) bytes or more, or None."""
     t, k = shape = a.shape
-    rows = n if n else w.shape[0]
+    rows = n if n else w.shape[0] if w.dim() == 2 else -1
     if residual is not None and epilogue in (0, 3):
         raise ValueError(f"relserve_linear_f8b: epilogue {epilogue} adds no residual")
     blocks = 2 * ((rows // 2 + 127) // 128) if epilogue == 3 else (rows + 127) // 128
@@ -613,15 +613,14 @@ def relserve_logprobs(logits, ids=None, logprobs=None, entropy=None, top_ids=Non
     """logits [rows, vocab] fp32 or bf16 (rows may be further apart: the first columns of a wider matrix); ids [rows, G] int32 and logprobs [rows, G]
     fp32; entropy [rows] fp32; top_ids [rows, k] int32 and top_logprobs [rows, k] fp32.  workspace: uint8 tensor of relserve_logprobs_workspace_bytes
     bytes or more, or None."""
-    rows, vocab = logits.shape
-    pitch, step = logits.stride()
     f32 = logits.dtype is torch.float32
-    if not (f32 or logits.dtype is torch.bfloat16) or (step != 1 and vocab > 1) or (pitch < vocab and rows > 1):
+    rows, vocab, pitch, step = (*logits.shape, *logits.stride()) if logits.dim() == 2 else (0, 0, 0, 0)
+    if logits.dim() != 2 or not (f32 or logits.dtype is torch.bfloat16) or (step != 1 and vocab > 1) or (pitch < vocab and rows > 1):
         raise ValueError(f"relserve_logprobs: logits must be rows of fp32 or bf16 entries one behind the other, not {logits.dtype} with strides "
                          f"{logits.stride()}")
     if (ids is None) != (logprobs is None) or (top_ids is None) != (top_logprobs is None):
         raise ValueError("relserve_logprobs: ids and logprobs, top_ids and top_logprobs are given together")
-    n_ids, n_top = 0 if ids is None else ids.shape[1], 0 if top_ids is None else top_ids.shape[1]
+    n_ids, n_top = (0 if t is None else t.shape[1] if t.dim() == 2 else -1 for t in (ids, top_ids))   # (-1: no shape that a tensor has)
     _dense("relserve_logprobs", ("ids", ids, torch.int32, (rows, n_ids)), ("logprobs", logprobs, torch.float32, (rows, n_ids)),
            ("entropy", entropy, torch.float32, (rows,)), ("top_ids", top_ids, torch.int32, (rows, n_top)),
            ("top_logprobs", top_logprobs, torch.float32, (rows, n_top)),
