@@ -163,8 +163,9 @@ __device__ __forceinline__ void store8(const Args& p, int t, int n, int cols, co
         }
         uint16_t* to = static_cast<uint16_t*>(p.out) + o;
         const uint2 c = make_uint2(pack_bf16x2(a[0], a[1]), pack_bf16x2(a[2], a[3])), d = make_uint2(pack_bf16x2(b[0], b[1]), pack_bf16x2(b[2], b[3]));
+        typedef uint32_t u32_quad __attribute__((ext_vector_type(4), aligned(8)));   // (rows of N % 8 = 4 outputs: every other one begins 8 bytes further)
         if (second)
-            *reinterpret_cast<uint4*>(to) = make_uint4(c.x, c.y, d.x, d.y);
+            *reinterpret_cast<u32_quad*>(to) = u32_quad{c.x, c.y, d.x, d.y};
         else
             *reinterpret_cast<uint2*>(to) = c;
     }
