@@ -642,8 +642,8 @@ hipError_t finish(const Args& p, int splits, hipStream_t s) {
     return hipGetLastError();
 }
 
-// How a projection runs: a tile, and into how many ranges k is cut.
-struct Plan { int tile, splits; };
+// How a projection runs: a tile, into how many ranges k is cut, and whether its weights go past the caches.
+struct Plan { int tile, splits; bool streamed; };
 enum { ROWS_16, ROWS_16_NARROW, ROWS_32, ROWS_32_NARROW, ROWS_64, TILE_64, TILE_128, TILE_128_WIDE, TILE_256, PLANS };
 
 // What a tile takes, in us: a launch's base, then for each round of workgroups over the chip its begin and end and its k steps (of a wave's own slices
@@ -669,6 +669,11 @@ double cost_of(const Args& p, bool wide, int tile, int splits) {
     return c.base + std::max(work, bytes / 4.5e6) + (splits > 1 ? 2.0 + splits * out * 4 / 6e6 + out * 6 / 5e6 : out * 4 / 20e6);
 }
 
+// Up to 16 tokens weights of 32 MB and more are read with the non-temporal hint: two layers with such a matrix are more than the last-level cache holds, so
+// that the next step finds them in memory.  us without -> with, from memory (from the cache): T = 1, 15360 x 5120 15.2 -> 14.2 (13.2, 13.2), SwiGLU 27648 x
+// 5120 26.3 -> 24.1, T = 16, 12288 x 4096 12.7 -> 12.1 (9.8 -> 10.7).  At 24 tokens it loses more from the cache than it gains (15360 x 5120 18.1 -> 17.7, 14.0 -> 16.2).
+constexpr int64_t kFarWeights = (int64_t)32 << 20;
+
 Plan plan_for(const Args& p, int epi) {
     const bool swiglu = epi == EPI_SWIGLU, wide = epi == EPI_RES_BF16_OUT_F32;
     const int64_t out = (int64_t)p.T * p.N;
@@ -684,7 +689,7 @@ Plan plan_for(const Args& p, int epi) {
             default: return p.T > 64;
         }
     };
-    Plan best{ROWS_32, 1};
+    Plan best{ROWS_32, 1, false};
     double least = 1e30;
     for (int tile = 0; tile < PLANS; ++tile) {
         if (!fits(tile)) continue;
@@ -692,23 +697,17 @@ Plan plan_for(const Args& p, int epi) {
             // (a range of gate rows and one of up rows in one tile of partial sums: where both end with a block)
             if (splits > 1 && (!p.slabs || splits * 2 > p.K / KB || splits * out > kSlabFloats || (swiglu && p.n_half % KB))) break;
             const double us = cost_of(p, wide, tile, splits);
-            if (us < least) least = us, best = {tile, splits};
+            if (us < least) least = us, best = {tile, splits, tile == ROWS_16 && (int64_t)p.N * p.K >= kFarWeights};
         }
     }
     return best;
 }
 
-// Up to 16 tokens weights of 32 MB and more are read with the non-temporal hint: two layers with such a matrix are more than the last-level cache holds, so
-// that the next step finds them in memory.  us without -> with, from memory (from the cache): T = 1, 15360 x 5120 15.2 -> 14.2 (13.2, 13.2), SwiGLU 27648 x
-// 5120 26.3 -> 24.1, T = 16, 12288 x 4096 12.7 -> 12.1 (9.8 -> 10.7).  At 24 tokens it loses more from the cache than it gains (15360 x 5120 18.1 -> 17.7, 14.0 -> 16.2).
-constexpr int64_t kFarWeights = (int64_t)32 << 20;
-
 template <int EPI, bool WIDE>
 hipError_t run_tile(const Args& p, Plan plan, hipStream_t s) {
     switch (plan.tile) {
         case ROWS_16:
-            return (int64_t)p.N * p.K >= kFarWeights ? launch_rows<EPI, 2, 1, 4, 3, WIDE, true>(p, plan.splits, s)
-                                                     : launch_rows<EPI, 2, 1, 4, 3, WIDE, false>(p, plan.splits, s);
+            return plan.streamed ? launch_rows<EPI, 2, 1, 4, 3, WIDE, true>(p, plan.splits, s) : launch_rows<EPI, 2, 1, 4, 3, WIDE, false>(p, plan.splits, s);
         case ROWS_16_NARROW:
             if constexpr (EPI != EPI_SWIGLU) return launch_rows<EPI, 1, 1, 4, 4, WIDE, false>(p, plan.splits, s);
             else return hipErrorInvalidValue;
@@ -753,7 +752,7 @@ GemmPlanF8b gemm_plan_f8b(int32_t T, int32_t N, int32_t K, int32_t epilogue, boo
     p.slabs = scratch ? &some_scratch : nullptr;
     const Plan plan = plan_for(p, epilogue);
     const int per_range = (K / KB + plan.splits - 1) / plan.splits;
-    return {plan.tile, (K / KB + per_range - 1) / per_range};
+    return {plan.tile, (K / KB + per_range - 1) / per_range, plan.streamed};
 }
 
 hipError_t launch_linear_f8b(const void* a, const float* a_scale, const void* w, const float* w_scale, int32_t T, int32_t N, int32_t K,

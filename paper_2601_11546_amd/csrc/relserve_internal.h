@@ -220,8 +220,9 @@ hipError_t launch_add_rmsnorm_f8b(const void* x, bool x_is_f32, const void* delt
 // launch_linear on such codes: a [T, K] with a_scale [K / 128, T], w [N, K] with w_scale [blocks of 128 rows, K / 128].  scratch: null, or
 // gemm_f8b_scratch_floats(T, N) floats, contents irrelevant on entry: k is cut into ranges where that pays
 int64_t gemm_f8b_scratch_floats(int64_t T, int64_t N);
-// How such a projection runs (host arithmetic alone): on the tile of that index (kernel_gemm_f8b.hip), k in that many ranges.
-struct GemmPlanF8b { int32_t tile, ranges; };
+// How such a projection runs (host arithmetic alone): on the tile of that index (kernel_gemm_f8b.hip), k in that many ranges, its weights past the
+// caches or not.
+struct GemmPlanF8b { int32_t tile, ranges, streamed; };
 GemmPlanF8b gemm_plan_f8b(int32_t T, int32_t N, int32_t K, int32_t epilogue, bool scratch);
 hipError_t launch_linear_f8b(const void* a, const float* a_scale, const void* w, const float* w_scale, int32_t T, int32_t N, int32_t K,
                              int32_t epilogue, const void* residual, void* out, hipStream_t s, float* scratch, bool w_packed);

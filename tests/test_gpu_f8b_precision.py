@@ -138,11 +138,9 @@ def test_before_the_rounding(rs, t, n, k, family):
     assert bool(((off[at] - (cut - y[at])).abs() <= tol).all()), float(((off[at] - (cut - y[at])).abs() / tol).max())
 
 
-@pytest.mark.parametrize("size", [s for s in f8b_paths.SIZES if s[3] != 1], ids=str)
-def test_paths(rs, size):
-    """Every tile's outputs in bf16: each one a rounding of the formula on cut products, off by fp32's roundings alone."""
+def check_path(rs, size):
+    """Outputs in bf16, each one a rounding of the formula on cut products, off by fp32's roundings alone."""
     t, n, k, epilogue = size
-    print(f"[case] precision of {f8b_paths.SIZES[size]}: {size}", flush=True)
     g = _gen(t + n + k)
     p = _problem(rs, g, "codes", t, n, k, epilogue)
     residual = _randn(g, t, n) if epilogue == 2 else None
@@ -166,6 +164,13 @@ def test_paths(rs, size):
     low, high = ((y + d).to(torch.bfloat16).double() for d in (-tol, tol))
     bad = (got < low) | (got > high)
     assert not bool(bad.any()), f"{int(bad.sum())} of {bad.numel()}"
+
+
+@pytest.mark.parametrize("size", [s for s in f8b_paths.SIZES if s[3] != 1], ids=str)
+def test_paths(rs, size):
+    """Every tile that writes bf16."""
+    print(f"[case] precision of {f8b_paths.SIZES[size]}: {size}", flush=True)
+    check_path(rs, size)
 
 
 @pytest.mark.parametrize("family", FAMILIES)
