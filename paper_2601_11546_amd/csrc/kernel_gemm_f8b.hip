@@ -20,6 +20,7 @@
 #include <type_traits>
 
 #include "device_utils.h"
+#include "gemm_tiles.h"
 #include "relserve_internal.h"
 
 namespace relserve {
@@ -27,8 +28,6 @@ namespace relserve {
 namespace {
 
 constexpr int KB = 128;        // codes of a k step: a block, a slice of the packed weights, a row of a stage in the LDS
-constexpr int NUM_XCD = 8;
-constexpr int GROUP_M = 8;
 
 enum { EPI_BF16 = 0, EPI_RES_BF16_OUT_F32 = 1, EPI_RES_F32_OUT_BF16 = 2, EPI_SWIGLU = 3, EPI_SLAB = 4 };
 
@@ -46,21 +45,7 @@ struct Args {
     int32_t per_split;       // k steps of a split (EPI_SLAB)
 };
 
-__device__ __forceinline__ const char* uniform_ptr(const char* ptr) {
-    const uint64_t v = reinterpret_cast<uint64_t>(ptr);
-    const uint32_t lo = __builtin_amdgcn_readfirstlane((uint32_t)v), hi = __builtin_amdgcn_readfirstlane((uint32_t)(v >> 32));
-    return reinterpret_cast<const char*>(((uint64_t)hi << 32) | lo);
-}
-
-// 64 lanes x 16 bytes from base + the lane's offset to 1 KB of LDS at lds_addr + at; one instruction has to stand between m0's write and the load.
-template <bool NT = false>
-__device__ __forceinline__ void dma16(const void* base, uint32_t voff, uint32_t lds_addr, int at) {
-    if (NT)
-        asm volatile("s_add_u32 m0, %2, %3\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1 nt" ::"v"(voff), "s"(base), "s"(lds_addr), "i"(at) : "memory", "scc");
-    else
-        asm volatile("s_add_u32 m0, %2, %3\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(voff), "s"(base), "s"(lds_addr), "i"(at) : "memory", "scc");
-}
-// 64 lanes x 4 bytes
+// As dma16, 64 lanes x 4 bytes
 __device__ __forceinline__ void dma4(const void* base, uint32_t voff, uint32_t lds_addr, int at) {
     asm volatile("s_add_u32 m0, %2, %3\n\ts_nop 0\n\tglobal_load_lds_dword %0, %1" ::"v"(voff), "s"(base), "s"(lds_addr), "i"(at) : "memory", "scc");
 }
@@ -99,28 +84,6 @@ __device__ __forceinline__ f32x4_t block_sum(const Wide& w, const Wide& a) {
 
 typedef const i32x4_t __attribute__((address_space(3))) * lds_chunk;
 typedef const float __attribute__((address_space(3))) * lds_float;
-
-// Consecutive workgroups go to different XCDs: each XCD's run of tiles is made contiguous, token tiles fastest within panels of GROUP_M.
-__device__ __forceinline__ int remap_xcd(int bid, int num) {
-    const int per = num / NUM_XCD, rem = num % NUM_XCD, xcd = bid % NUM_XCD, idx = bid / NUM_XCD;
-    return xcd < rem ? xcd * (per + 1) + idx : rem * (per + 1) + (xcd - rem) * per + idx;
-}
-__device__ __forceinline__ void tile_coords(int t, int tiles_m, int tiles_n, int& tile_m, int& tile_n) {
-    const int panels = (tiles_m + GROUP_M - 1) / GROUP_M, base = tiles_m / panels, extra = tiles_m % panels, big = (base + 1) * tiles_n;
-    int first, size, in;
-    if (t < extra * big) {
-        size = base + 1;
-        first = t / big * size;
-        in = t % big;
-    } else {
-        const int u = t - extra * big, per = base * tiles_n;
-        size = base;
-        first = extra * (base + 1) + u / per * base;
-        in = u % per;
-    }
-    tile_m = first + in % size;
-    tile_n = in / size;
-}
 
 // Row of the weights' scales that feature n's block has.
 __device__ __forceinline__ int scale_row(const Args& p, bool swiglu, int n, bool up) { return (swiglu && up ? (p.n_half + KB - 1) / KB : 0) + n / KB; }
@@ -417,8 +380,7 @@ hipError_t launch_tiles(Args p, int splits, hipStream_t s) {
     static std::once_flag once;
     static hipError_t st = hipSuccess;
     auto kernel = &tile_kernel<BM, BN, WM, WN, NS, EPI, WIDE>;
-    std::call_once(once, [&] { st = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, smem); });
-    if (st != hipSuccess) return st;
+    if (hipError_t e = allow_smem_once(once, st, kernel, smem)) return e;
     kernel<<<dim3((unsigned)(p.tiles_m * p.tiles_n * splits)), dim3(64 * WM * WN), smem, s>>>(p);
     return hipGetLastError();
 }
@@ -602,8 +564,7 @@ hipError_t launch_rows(Args p, int splits, hipStream_t s) {
     static std::once_flag once;
     static hipError_t st = hipSuccess;
     auto kernel = &rows_kernel<EPI, FN, TM, W, S, WIDE, NT>;
-    std::call_once(once, [&] { st = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, smem); });
-    if (st != hipSuccess) return st;
+    if (hipError_t e = allow_smem_once(once, st, kernel, smem)) return e;
     kernel<<<dim3((unsigned)(p.tiles_m * p.tiles_n * splits)), dim3(64 * W), smem, s>>>(p);
     return hipGetLastError();
 }
