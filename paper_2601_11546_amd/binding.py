@@ -418,6 +418,10 @@ def pack_layer_weights_w8a8(weights: dict) -> dict:
     return out
 
 
+# torch.cuda.current_device, without its question whether the runtime is up (a tensor lies on a device): 0.10 us a call, 0.18
+_current_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
+
+
 def _dense(where: str, *tensors, device=None) -> None:
     """The int8 and the block-scaled entry points take whole row-major matrices on the current device, of the types and shapes named: (name, tensor,
     dtype, shape).  device: where another operand lies."""
@@ -432,7 +436,7 @@ def _dense(where: str, *tensors, device=None) -> None:
             if device is not None:
                 raise ValueError(f"{where}: {name} lies on {t.device}, other tensors elsewhere")
             device = at
-    if device < 0 or device != torch.cuda.current_device():
+    if device < 0 or device != _current_device():
         raise ValueError(f"{where}: the tensors do not lie on the current device")
 
 
@@ -613,14 +617,21 @@ def relserve_logprobs(logits, ids=None, logprobs=None, entropy=None, top_ids=Non
     """logits [rows, vocab] fp32 or bf16 (rows may be further apart: the first columns of a wider matrix); ids [rows, G] int32 and logprobs [rows, G]
     fp32; entropy [rows] fp32; top_ids [rows, k] int32 and top_logprobs [rows, k] fp32.  workspace: uint8 tensor of relserve_logprobs_workspace_bytes
     bytes or more, or None."""
+    try:
+        (rows, vocab), (pitch, step) = logits.shape, logits.stride()
+    except ValueError:
+        rows, vocab, pitch, step = 0, 2, 0, 0   # no matrix: refused as one whose entries lie apart
     f32 = logits.dtype is torch.float32
-    rows, vocab, pitch, step = (*logits.shape, *logits.stride()) if logits.dim() == 2 else (0, 0, 0, 0)
-    if logits.dim() != 2 or not (f32 or logits.dtype is torch.bfloat16) or (step != 1 and vocab > 1) or (pitch < vocab and rows > 1):
+    if not (f32 or logits.dtype is torch.bfloat16) or (step != 1 and vocab > 1) or (pitch < vocab and rows > 1):
         raise ValueError(f"relserve_logprobs: logits must be rows of fp32 or bf16 entries one behind the other, not {logits.dtype} with strides "
                          f"{logits.stride()}")
     if (ids is None) != (logprobs is None) or (top_ids is None) != (top_logprobs is None):
         raise ValueError("relserve_logprobs: ids and logprobs, top_ids and top_logprobs are given together")
-    n_ids, n_top = (0 if t is None else t.shape[1] if t.dim() == 2 else -1 for t in (ids, top_ids))   # (-1: no shape that a tensor has)
+    try:
+        n_ids, n_top = 0 if ids is None else ids.shape[1], 0 if top_ids is None else top_ids.shape[1]
+    except IndexError:
+        name = "ids" if ids is not None and ids.dim() < 2 else "top_ids"
+        raise ValueError(f"relserve_logprobs: {name} must be a matrix") from None
     _dense("relserve_logprobs", ("ids", ids, torch.int32, (rows, n_ids)), ("logprobs", logprobs, torch.float32, (rows, n_ids)),
            ("entropy", entropy, torch.float32, (rows,)), ("top_ids", top_ids, torch.int32, (rows, n_top)),
            ("top_logprobs", top_logprobs, torch.float32, (rows, n_top)),
