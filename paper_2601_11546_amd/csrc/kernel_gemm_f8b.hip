@@ -126,7 +126,8 @@ __device__ __forceinline__ void store8(const Args& p, int t, int n, int cols, co
         }
         uint16_t* to = static_cast<uint16_t*>(p.out) + o;
         const uint2 c = make_uint2(pack_bf16x2(a[0], a[1]), pack_bf16x2(a[2], a[3])), d = make_uint2(pack_bf16x2(b[0], b[1]), pack_bf16x2(b[2], b[3]));
-        typedef uint32_t u32_quad __attribute__((ext_vector_type(4), aligned(8)));   // (rows of N % 8 = 4 outputs: every other one begins 8 bytes further)
+        // rows of N % 8 = 4 outputs: every other one begins 8 bytes further (as a uint4 it is also taken apart into four stores: 1282 x 15360 x 5120 114 us, 124)
+        typedef uint32_t u32_quad __attribute__((ext_vector_type(4), aligned(8)));
         if (second)
             *reinterpret_cast<u32_quad*>(to) = u32_quad{c.x, c.y, d.x, d.y};
         else
@@ -609,9 +610,12 @@ enum { ROWS_16, ROWS_16_NARROW, ROWS_32, ROWS_32_NARROW, ROWS_64, TILE_64, TILE_
 
 // What a tile takes, in us: a launch's base, then for each round of workgroups over the chip its begin and end and its k steps (of a wave's own slices
 // for rows), both of codes and of codes widened to bf16; a step of a round that leaves CUs idle costs `alone` of that, the rest by how many work.
-// Fitted to measured launches, weights from memory: 4200 of 129 shapes of 1 .. 8192 tokens, and for widened codes 2700 of 116 shapes of 33 .. 4099.  The
-// plans chosen by it are 2.7 % slower than the best one of each shape on average, 37 % at worst (700 x 612 x 2560: 15.6 us for 11.4); of the
-// second set 0.9 % and 16 % (128 x 5120 x 5120 onto fp32: 22.4 us for 19.2).
+// Fitted to measured launches, weights from memory, fp32 outputs above 32 tokens apart from the rest.  Against the best plan of each of 326 shapes (6139 launches,
+// weights from memory) the chosen one is slower by, on average and at worst: bf16 outputs and SwiGLU 2.4 %, 39 % (24 x 4096 x 14336: 21.7 us for 15.6 in
+// ROWS_32_NARROW); fp32 outputs above 32 tokens 2.8 %, 26 % (2050 x 4096 x 4096: 113 for 90 in TILE_64), of 17..32 tokens 4.4 %, 27 %, of up to 16 tokens
+// 12.3 %, 43 % (1 x 640 x 7552: 9.3 for 6.5).  The last is ROWS_16_NARROW's step_wide, which no launch stands behind: a step takes it 0.25 .. 0.35 us, and with 5.66 it is
+// chosen at k = 128 alone, where fp32 outputs of up to 128 workgroups would gain by it (4 x 4096 x 4096 7.0 -> 6.1 us, 4 x 2560 x 5120 7.4 -> 5.8,
+// 4 x 1024 x 4096 5.5 -> 4.7).
 struct TileCost { int rows, features, at_once; double base, step, step_wide, round, round_wide, alone; };
 constexpr TileCost kCost[PLANS] = {
     {16, 32, 512, 0.11, 1.17, 0.79, 1.63, 1.63, 0.19},  {16, 16, 768, 0.14, 0.53, 5.66, 1.29, 1.29, 0.18},  {32, 32, 512, 2.45, 1.52, 0.94, 1.22, 0.78, 0.10},
@@ -641,8 +645,11 @@ Plan plan_for(const Args& p, int epi) {
     auto fits = [&](int tile) {
         switch (tile) {
             case ROWS_16: return p.T <= 16;
-            case ROWS_16_NARROW: return !swiglu && p.T <= 16 && (p.N + 31) / 32 < 160;   // where 32 features each leave CUs idle
+            // 16 features each where that many more workgroups find idle CUs.  us in 32 and in 16, 4 tokens, bf16 outputs, weights from memory: 32 workgroups (of 32
+            // features; k = 4096) 4.6, 4.0; 80 (5120) 7.0, 5.4; 128 (4096) 6.5, 5.8; 160 (5120) 7.6, 8.3, (13824) 14.2, 17.4; 192 (4096) 7.2, 7.7
+            case ROWS_16_NARROW: return !swiglu && p.T <= 16 && (p.N + 31) / 32 < 160;
             case ROWS_32: return p.T <= 128;
+            // the same, 24 tokens: 32 workgroups 5.5, 4.8; 80 9.2, 7.9; 160 9.8, 12.0 ((13824) 19.6, 24.1); 128, which it leaves out, 8.1, 6.9 ((14336) 19.5, 15.5)
             case ROWS_32_NARROW: return !swiglu && p.T > 16 && p.T <= 128 && (p.N + 31) / 32 * ((p.T + 31) / 32) < 128;
             case ROWS_64: return p.T > 32 && p.T <= 512;
             case TILE_64: return p.T > 32;
