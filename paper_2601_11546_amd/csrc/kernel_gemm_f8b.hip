@@ -610,9 +610,9 @@ enum { ROWS_16, ROWS_16_NARROW, ROWS_32, ROWS_32_NARROW, ROWS_64, TILE_64, TILE_
 
 // What a tile takes, in us: a launch's base, then for each round of workgroups over the chip its begin and end and its k steps (of a wave's own slices
 // for rows), both of codes and of codes widened to bf16; a step of a round that leaves CUs idle costs `alone` of that, the rest by how many work.
-// Fitted to measured launches, weights from memory, fp32 outputs above 32 tokens apart from the rest.  Against the best plan of each of 326 shapes (6139 launches,
+// Fitted to measured launches, weights from memory, fp32 outputs above 32 tokens apart from the rest.  Against the best plan of each of 325 shapes (6125 launches,
 // weights from memory) the chosen one is slower by, on average and at worst: bf16 outputs and SwiGLU 2.4 %, 39 % (24 x 4096 x 14336: 21.7 us for 15.6 in
-// ROWS_32_NARROW); fp32 outputs above 32 tokens 2.8 %, 26 % (2050 x 4096 x 4096: 113 for 90 in TILE_64), of 17..32 tokens 4.4 %, 27 %, of up to 16 tokens
+// ROWS_32_NARROW); fp32 outputs above 32 tokens 2.8 %, 26 % (2050 x 4096 x 4096: 113 for 90 in TILE_64), of 17..32 tokens 4.5 %, 27 %, of up to 16 tokens
 // 12.3 %, 43 % (1 x 640 x 7552: 9.3 for 6.5).  The last is ROWS_16_NARROW's step_wide, which no launch stands behind: a step takes it 0.25 .. 0.35 us, and with 5.66 it is
 // chosen at k = 128 alone, where fp32 outputs of up to 128 workgroups would gain by it (4 x 4096 x 4096 7.0 -> 6.1 us, 4 x 2560 x 5120 7.4 -> 5.8,
 // 4 x 1024 x 4096 5.5 -> 4.7).
