@@ -302,7 +302,8 @@ int32_t relserve_greedy_sample(const void* logits, int32_t n_rows, int32_t vocab
  * natural logarithms, top_ids[r, 0 .. n_top) the entries with the largest logits in falling order, the lowest id first among equal ones, and
  * top_logprobs their log p.  Entries of -infinity have probability 0; a row with a NaN or an infinity, or with no entry above -infinity, has NaN for its
  * log probabilities and entropy, while its alternatives are ordered all the same; NaN entries are no alternatives; behind the last entry of a row stand
- * id -1 and -infinity.  Sums in fp32, their largest term held apart, so that a log probability next to 0 keeps its digits.
+ * id -1 and -infinity.  Sums in fp32, their largest term held apart, so that a log probability next to 0 keeps its digits; off by some sixty roundings
+ * of fp32 at most and one more for each 8192 entries of a row.
  * logits: device, fp32 (logits_are_f32 != 0) or bf16, row r begins at element r * pitch (pitch >= vocab: columns behind the vocabulary are not read).
  * ids [n_rows, n_ids], logprobs [n_rows, n_ids] fp32, entropy [n_rows] fp32 (or NULL), top_ids [n_rows, n_top], top_logprobs [n_rows, n_top] fp32; n_ids
  * and n_top may be 0 (with NULL arrays), n_top at most 32.  n_rows at most 2^22, vocab 2^24 (RELSERVE_ERR_TOO_LARGE).  workspace: scratch as in
